@@ -49,7 +49,9 @@ typedef enum {
   MARLIN_ERR_WORKSPACE = 5,      /* workspace smaller than marlin_workspace_bytes()             */
   MARLIN_ERR_ARCH = 6,           /* current device is not sm_100                                */
   MARLIN_ERR_CUDA = 7,           /* a CUDA runtime call or the launch failed                    */
-  MARLIN_ERR_DEVICE_TIMEOUT = 8  /* a bounded wait inside a kernel expired (see marlin_read_status) */
+  MARLIN_ERR_DEVICE_TIMEOUT = 8, /* a bounded wait inside a kernel expired (see marlin_read_status) */
+  MARLIN_ERR_CACHE = 9           /* a length or a page number points outside of the cache: kernels report it through
+                                    marlin_read_status, and leave out what it would have reached */
 } marlin_status;
 
 /* A CUDA stream handle (cudaStream_t) passed as an opaque pointer; NULL is the default stream. */
@@ -243,8 +245,101 @@ MARLIN_API int marlin_gemm_sparse24(const void* A, const void* w_packed, const v
                          const void* s_packed, void* C, int M, int K, int N, int group_size,
                          void* workspace, size_t workspace_bytes, marlin_stream stream);
 
+/* ---- the paged key-value cache: the part of a decoder layer between the qkv layer and the output layer -----------
+ *
+ * Section 5.2 of the paper measures these layers inside a serving engine; there the tokens that a sequence has so far
+ * are kept as keys and values in pages of a fixed number of tokens, handed out in any order. */
+
+#define MARLIN_KV_FP16 0  /* cache elements are fp16 */
+#define MARLIN_KV_E4M3 1  /* cache elements are 8-bit floats (4 exponent and 3 mantissa bits, largest 448), and stand for
+                             their value times k_scale[head] or v_scale[head] */
+
+/* A cache and its tables (a host structure of device pointers; the library keeps none of it after a call).
+ * Element d of head h of the token at position p of sequence b lies in k (and in v) at
+ *   table[b * table_stride + p / page_size] * stride[0] + h * stride[1] + (p % page_size) * stride[2] + d
+ * so [pages][heads][page_size][head_dim] and [pages][page_size][heads][head_dim] are both of this form.  Strides count
+ * elements and are multiples of 16 bytes; k and v (16-byte aligned, or NULL nowhere) have the same ones.  No two of
+ * these places may overlap. */
+typedef struct {
+  void* k;                 /* device                                                                            */
+  void* v;                 /* device                                                                            */
+  int64_t stride[3];       /* elements between pages, heads and tokens                                          */
+  const int32_t* table;    /* device, [sequences][max_pages]: page numbers; entries behind a sequence's last page
+                              are not read                                                                      */
+  int64_t table_stride;    /* entries between sequences, >= max_pages                                           */
+  const int32_t* lengths;  /* device, [sequences]: tokens of each sequence, the new ones of the call included   */
+  const float* k_scale;    /* device, [kv_heads], or NULL (1); 8-bit caches only                                */
+  const float* v_scale;
+  int pages;               /* pages in k and v                                                                  */
+  int max_pages;           /* entries of a row of `table`                                                       */
+  int sequences;
+  int kv_heads;
+  int head_dim;            /* a multiple of 16, at most 256                                                     */
+  int page_size;           /* tokens, a power of two                                                            */
+  int format;              /* MARLIN_KV_FP16 or MARLIN_KV_E4M3                                                  */
+} marlin_kv_cache;
+
+/* The new tokens of a call: rows starts[b] .. starts[b + 1] - 1 of the inputs belong to sequence b, in the order of their
+ * positions, of which the last is lengths[b] - 1; `starts` is device, int32 [sequences + 1], not descending, its values
+ * in 0 .. tokens.  NULL: one token per sequence (tokens == sequences), row b for sequence b.  Rows in front of starts[0]
+ * and behind starts[sequences] belong to nobody: neither the cache nor their rows of the outputs are written.  A token whose position
+ * would be negative (a sequence with fewer tokens than rows, for example an empty one of a padded batch) is not put
+ * into the cache; its rows of the outputs are zeros.
+ * A length outside of 0 .. max_pages * page_size is taken as the nearest of the two, a page number outside of 0 .. pages - 1 as a page
+ * that is not there (nothing is written to it, attention reads zeros for it); both set the status word to MARLIN_ERR_CACHE. */
+
+/* Bytes of workspace of the three calls below on heads of head_dim elements (0: not supported; host arithmetic only).
+ * The workspace is that of marlin_workspace_bytes and under the same contract: zeroed once, the counters zero again
+ * after every call, one call at a time; one buffer of the largest size serves these calls and the layers. */
+MARLIN_API size_t marlin_attention_workspace_bytes(int head_dim);
+
+/* Puts the keys and values of new tokens into the cache and rotates queries and keys by their positions.
+ *   q, k, v    device, fp16: heads of one token side by side, q_heads (or kv_heads) * head_dim values, tokens q_stride,
+ *              k_stride, v_stride elements apart (multiples of 8): three column ranges of the output of one qkv layer,
+ *              or three tensors.  q may be NULL (and q_heads 0): only the cache is written.
+ *   q_out      device, out, fp16 [tokens][q_heads * head_dim]; NULL where q is
+ *   inv_freq   device, fp32 [rotary_dim / 2]: radians per position of each pair, or NULL: no rotation (then q must be NULL)
+ *   rotary_dim a multiple of 16, at most head_dim: the first rotary_dim elements of a head are rotated, in pairs
+ *              (j, j + rotary_dim / 2), or (2 j, 2 j + 1) where `interleaved` is set:
+ *                (a, c) -> (a cos t - c sin t, c cos t + a sin t),  t = position * inv_freq[j]
+ * Angles are formed in 64 bits and reduced by whole turns before sine and cosine are taken in fp32; the rotation is fp32
+ * and the result is rounded once (to nearest even; to e4m3 after division by the scale, saturating at 448, NaN kept). */
+MARLIN_API int marlin_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     void* q_out, const marlin_kv_cache* cache, const int32_t* starts, int tokens, int q_heads,
+                     const float* inv_freq, int rotary_dim, int interleaved,
+                     void* workspace, size_t workspace_bytes, marlin_stream stream);
+
+/* Attention of new tokens over the cache, which holds them already (marlin_kv_append).
+ *   q          device, fp16, q_heads * head_dim values per token, tokens q_stride elements apart (a multiple of 8); query
+ *              head h reads key head h / (q_heads / kv_heads), q_heads a multiple of kv_heads
+ *   scale      factor of the logits, usually 1 / sqrt(head_dim)
+ *   window     0, or the number of positions that a token sees, its own included (a sliding window)
+ *   out        device, out, fp16 [tokens][q_heads * head_dim]
+ * out = sum_j w_j v_j, w = softmax over the positions j <= p, j > p - window of scale * q . k_j, p the token's position;
+ * zeros where there is none.  Values at other positions never reach a result, whatever they are (infinities, NaN).
+ * One launch: the tiles of 64 keys of all sequences and key heads are numbered through and cut into equal ranges, one
+ * per CTA (the stripes of Section 3.4 "Striped Partitioning"); parts of a sequence are joined by the CTA that comes last,
+ * in the order of the keys, so that the same inputs give the same bits on every call.  Sums and the softmax are fp32.
+ * Any number of tokens per sequence is right; it is made for one and the few of speculative decoding (bound by reading the cache). */
+MARLIN_API int marlin_attention_decode(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const int32_t* starts,
+                            int tokens, int q_heads, float scale, int window, void* out,
+                            void* workspace, size_t workspace_bytes, marlin_stream stream);
+
+/* The attention half of a decoder layer as a chain of four launches (marlin_mlp_swiglu is the other half): QKV = A . W_qkv,
+ * marlin_kv_append of its columns (q_heads, then kv_heads keys, then kv_heads values), marlin_attention_decode, C = O . W_o.
+ *   A       device, fp16 [M][K], M tokens;  W_qkv: K x (q_heads + 2 kv_heads) * head_dim, W_o: q_heads * head_dim x N
+ *   QKV, Q, O   device scratch, fp16 [M][(q_heads + 2 kv_heads) * head_dim], [M][q_heads * head_dim] twice.  Q may be NULL
+ *           where inv_freq is.  Rows of O that belong to no sequence are not written, and go through W_o as they are.
+ *   workspace   the largest of marlin_workspace_bytes of both layers and marlin_attention_workspace_bytes.
+ * All arguments are checked before anything is queued. */
+MARLIN_API int marlin_attention_block(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o,
+                           void* QKV, void* Q, void* O, void* C, const marlin_kv_cache* cache, const int32_t* starts,
+                           int M, int K, int q_heads, int N, int group_size, const float* inv_freq, int rotary_dim,
+                           int interleaved, float scale, int window,
+                           void* workspace, size_t workspace_bytes, marlin_stream stream);
+
 /* Synchronises `stream`, then returns the device-side status word of `workspace`
- * (MARLIN_OK, or MARLIN_ERR_DEVICE_TIMEOUT if a kernel gave up a bounded wait), or
+ * (MARLIN_OK, MARLIN_ERR_DEVICE_TIMEOUT if a kernel gave up a bounded wait, or MARLIN_ERR_CACHE), or
  * MARLIN_ERR_CUDA if the stream reports an error.  The status word is sticky until the
  * workspace is zeroed again. */
 MARLIN_API int marlin_read_status(const void* workspace, marlin_stream stream);

@@ -5,14 +5,19 @@ The product is the C-ABI library ``libmarlin_b200.so`` declared in ``include/mar
 call loads the library and raises if it is missing (there is no CPU or eager fallback).
 """
 from .binding import (  # noqa: F401
+    KvCache,
     Layer,
     MarlinError,
+    attention_block,
+    attention_decode,
+    attention_workspace_bytes,
     gemm,
     gemm_sparse24,
     gemm_static_ws,
     gemm_swiglu,
     gemm_w8,
     interleave_gate_up,
+    kv_append,
     gemm_zp,
     lib,
     mlp_swiglu,

@@ -21,6 +21,7 @@ EXPORTS = [
     "marlin_gemm_static_ws", "marlin_quantize_rtn", "marlin_pack_zeros", "marlin_unpack_zeros", "marlin_gemm_zp",
     "marlin_interleave_gate_up", "marlin_gemm_swiglu", "marlin_mlp_swiglu",
     "marlin_packed_weight_bytes_w8", "marlin_pack_w8", "marlin_unpack_w8", "marlin_gemm_w8",
+    "marlin_attention_workspace_bytes", "marlin_kv_append", "marlin_attention_decode", "marlin_attention_block",
 ]
 STATIC_WS_MAX_M = 16  # MARLIN_STATIC_WS_MAX_M of the header
 
@@ -77,9 +78,15 @@ def lib():
     L.marlin_pack_sparse24.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, vp]
     L.marlin_unpack_sparse24.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, vp]
     L.marlin_gemm_sparse24.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, vp, sz, vp]
+    L.marlin_attention_workspace_bytes.restype = sz
+    L.marlin_attention_workspace_bytes.argtypes = [i]
+    i64, f32 = c.c_int64, c.c_float
+    L.marlin_kv_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i, i, vp, i, i, vp, sz, vp]
+    L.marlin_attention_decode.argtypes = [vp, i64, vp, vp, i, i, f32, i, vp, vp, sz, vp]
+    L.marlin_attention_block.argtypes = [vp] * 11 + [i] * 5 + [vp, i, i, f32, i, vp, sz, vp]
     L.marlin_read_status.argtypes = [vp, vp]
     L.marlin_plan_stripes.argtypes = [i, i, i, i, vp, vp, vp, i]
-    for name in ("marlin_pack_w8", "marlin_unpack_w8", "marlin_gemm_w8", "marlin_interleave_gate_up", "marlin_gemm_swiglu", "marlin_mlp_swiglu", "marlin_pack_zeros", "marlin_unpack_zeros", "marlin_gemm_zp", "marlin_quantize_rtn", "marlin_gemm_static_ws", "marlin_pack", "marlin_unpack", "marlin_gemm", "marlin_pack_sparse24", "marlin_unpack_sparse24",
+    for name in ("marlin_kv_append", "marlin_attention_decode", "marlin_attention_block", "marlin_pack_w8", "marlin_unpack_w8", "marlin_gemm_w8", "marlin_interleave_gate_up", "marlin_gemm_swiglu", "marlin_mlp_swiglu", "marlin_pack_zeros", "marlin_unpack_zeros", "marlin_gemm_zp", "marlin_quantize_rtn", "marlin_gemm_static_ws", "marlin_pack", "marlin_unpack", "marlin_gemm", "marlin_pack_sparse24", "marlin_unpack_sparse24",
                  "marlin_gemm_sparse24", "marlin_read_status", "marlin_plan_stripes"):
         getattr(L, name).restype = i
     _lib = L
@@ -392,6 +399,60 @@ def gemm_sparse24(A, w_packed, meta_packed, s_packed, K: int, N: int, group_size
                   stream=None):
     """marlin_gemm_sparse24: C = A . W for a 2:4 layer (see pack_sparse24)."""
     return native().gemm(_SPARSE, A, w_packed, s_packed, meta_packed, K, N, group_size, workspace, out, stream)
+
+
+class KvCache(ctypes.Structure):
+    """marlin_kv_cache of the header, for callers of the C ABI."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride", ctypes.c_int64 * 3), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("lengths", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int), ("max_pages", ctypes.c_int), ("sequences", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int), ("format", ctypes.c_int)]
+
+
+def attention_workspace_bytes(head_dim: int) -> int:
+    n = int(lib().marlin_attention_workspace_bytes(head_dim))
+    if n == 0:
+        raise MarlinError(2, "marlin_attention_workspace_bytes")
+    return n
+
+
+def kv_append(qkv, k_cache, v_cache, pages, lengths, workspace, inv_freq=None, interleaved: bool = False, starts=None,
+              k_scale=None, v_scale=None, out=None, stream=None):
+    """marlin_kv_append: puts the keys and values of new tokens into a paged cache and rotates queries and keys.
+
+    qkv       fp16 [T, (q_heads + 2 kv_heads) * head_dim], as the qkv layer leaves it: queries, keys, values
+    k_cache, v_cache   fp16 or float8_e4m3fn [pages, kv_heads, page_size, head_dim], any strides but the last
+    pages     int32 [B, max_pages]: the pages of each sequence
+    lengths   int32 [B]: tokens of each sequence, the new ones included
+    workspace uint8, attention_workspace_bytes(head_dim), zeroed once (a layer's workspace serves if it is large enough)
+    inv_freq  fp32 [rotary_dim / 2], or None: no rotation;  interleaved: pairs are (2 j, 2 j + 1), not (j, j + rotary_dim / 2)
+    starts    int32 [B + 1]: sequence b has the rows starts[b] .. starts[b + 1] - 1; None: one row each
+    k_scale, v_scale   fp32 [kv_heads] of an 8-bit cache, or None: 1
+
+    Returns the rotated queries [T, q_heads * head_dim]; without inv_freq the columns of qkv that hold them."""
+    return native().kv_append(qkv, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, inv_freq,
+                              interleaved, out)
+
+
+def attention_decode(q, k_cache, v_cache, pages, lengths, workspace, scale=None, window: int = 0, starts=None, k_scale=None,
+                     v_scale=None, out=None, stream=None):
+    """marlin_attention_decode: attention of new tokens over a paged cache that holds them already (see kv_append).
+
+    q         fp16 [T, q_heads * head_dim], possibly a range of columns;  scale: 1 / sqrt(head_dim) unless given
+    window    0, or the number of positions that a token sees, its own included
+
+    Returns fp16 [T, q_heads * head_dim]; rows that belong to no sequence are not written."""
+    return native().attention_decode(q, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, scale,
+                                     window, out)
+
+
+def attention_block(A, w_qkv, s_qkv, w_o, s_o, k_cache, v_cache, pages, lengths, K: int, q_heads: int, N: int, group_size: int,
+                    workspace, inv_freq=None, interleaved: bool = False, scale=None, window: int = 0, starts=None, k_scale=None,
+                    v_scale=None, QKV=None, Q=None, O=None, out=None, stream=None):
+    """marlin_attention_block: the qkv layer, kv_append, attention_decode and the output layer as four launches; returns
+    C [M, N].  QKV, Q and O are scratch (taken from torch's allocator unless given)."""
+    return native().attention_block(A, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, inv_freq,
+                                    interleaved, scale, window, w_qkv, s_qkv, w_o, s_o, K, q_heads, N, group_size, QKV, Q, O, out)
 
 
 class Layer:

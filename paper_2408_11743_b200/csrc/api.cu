@@ -85,6 +85,7 @@ const char* marlin_status_string(int status) {
     case MARLIN_ERR_ARCH: return "device is not sm_100";
     case MARLIN_ERR_CUDA: return "CUDA error";
     case MARLIN_ERR_DEVICE_TIMEOUT: return "bounded wait expired inside a kernel";
+    case MARLIN_ERR_CACHE: return "a length or a page number outside of the cache";
     default: return "unknown status";
   }
 }
@@ -433,6 +434,177 @@ int marlin_gemm_sparse24(const void* A, const void* w_packed, const void* meta_p
                          marlin_stream stream) {
   return gemm_common(A, w_packed, meta_packed, s_packed, C, M, K, N, group_size, workspace, workspace_bytes, stream,
                      true);
+}
+
+// ---- the paged key-value cache ------------------------------------------------------------------
+size_t marlin_attention_workspace_bytes(int head_dim) {
+  if (head_dim < 16 || head_dim > 256 || head_dim % 16) return 0;
+  return kWsPartialOff + attention_slot_bytes(head_dim);
+}
+
+// The checks that both calls make of the cache, the tokens and the workspace; on success the cache as the kernels see it.
+static int check_cache(const marlin_kv_cache* c, const int32_t* starts, int tokens, int q_heads, const void* workspace,
+                       size_t workspace_bytes, KvCacheView* view) {
+  if (!c || !c->k || !c->v || !c->table || !c->lengths || !workspace) return MARLIN_ERR_NULL;
+  const size_t need = marlin_attention_workspace_bytes(c->head_dim);
+  const bool eight_bit = c->format == MARLIN_KV_E4M3;
+  if (!need || (!eight_bit && c->format != MARLIN_KV_FP16) || c->page_size < 1 || (c->page_size & (c->page_size - 1)) ||
+      c->pages < 1 || c->max_pages < 1 || c->table_stride < c->max_pages || c->kv_heads < 1 || c->kv_heads > 65536 || c->sequences < 1 ||
+      tokens < 1 || (!starts && tokens != c->sequences) || q_heads < 0 || q_heads > 65536 || q_heads % c->kv_heads ||
+      (long long)tokens * (q_heads / c->kv_heads) > (1ll << 30))  // (rows of a key head are numbered in 32 bits)
+    return MARLIN_ERR_SHAPE;
+  const int vector = eight_bit ? 16 : 8;  // elements of 16 bytes
+  for (int i = 0; i < 3; ++i) {
+    if (c->stride[i] < 0) return MARLIN_ERR_SHAPE;
+    if (c->stride[i] % vector) return MARLIN_ERR_ALIGN;
+  }
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(workspace)) return MARLIN_ERR_ALIGN;
+  // tables of 4-byte numbers may begin in the middle of a larger one
+  const uintptr_t numbers = reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->lengths) |
+                            reinterpret_cast<uintptr_t>(starts) | reinterpret_cast<uintptr_t>(c->k_scale) |
+                            reinterpret_cast<uintptr_t>(c->v_scale);
+  if (numbers & 3) return MARLIN_ERR_ALIGN;
+  if (!eight_bit && (c->k_scale || c->v_scale)) return MARLIN_ERR_SHAPE;  // a scale that would not be applied
+  if (workspace_bytes < need) return MARLIN_ERR_WORKSPACE;
+  view->k = c->k;
+  view->v = c->v;
+  view->s_page = c->stride[0];
+  view->s_head = c->stride[1];
+  view->s_token = c->stride[2];
+  view->table = c->table;
+  view->table_stride = c->table_stride;
+  view->lengths = c->lengths;
+  view->k_scale = c->k_scale;
+  view->v_scale = c->v_scale;
+  view->pages = c->pages;
+  view->max_pages = c->max_pages;
+  view->sequences = c->sequences;
+  view->kv_heads = c->kv_heads;
+  view->head_dim = c->head_dim;
+  view->page_shift = 0;
+  while ((1 << view->page_shift) < c->page_size) ++view->page_shift;
+  view->eight_bit = eight_bit;
+  return MARLIN_OK;
+}
+
+static int device_is_ours(int* sm_count) {
+  DeviceInfo info;
+  const int st = device_info(&info);
+  if (st != MARLIN_OK) return st;
+  *sm_count = info.sm_count;
+  return info.cc_major == 10 ? MARLIN_OK : MARLIN_ERR_ARCH;
+}
+
+static int check_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                        void* q_out, const marlin_kv_cache* cache, const int32_t* starts, int tokens, int q_heads,
+                        const float* inv_freq, int rotary_dim, void* workspace, size_t workspace_bytes, AppendParams* p) {
+  if (!k || !v || (q_heads > 0 && (!q || !q_out))) return MARLIN_ERR_NULL;
+  const int st = check_cache(cache, starts, tokens, q_heads, workspace, workspace_bytes, &p->cache);
+  if (st != MARLIN_OK) return st;
+  if (q_stride < 0 || k_stride < 0 || v_stride < 0 || (q_heads > 0 && !inv_freq) ||
+      (inv_freq && (rotary_dim < 16 || rotary_dim % 16 || rotary_dim > cache->head_dim)))
+    return MARLIN_ERR_SHAPE;
+  if (q_stride % 8 || k_stride % 8 || v_stride % 8 || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) ||
+      (reinterpret_cast<uintptr_t>(inv_freq) & 3))
+    return MARLIN_ERR_ALIGN;
+  p->q = static_cast<const uint16_t*>(q);
+  p->k = static_cast<const uint16_t*>(k);
+  p->v = static_cast<const uint16_t*>(v);
+  p->q_stride = q_stride;
+  p->k_stride = k_stride;
+  p->v_stride = v_stride;
+  p->q_out = static_cast<uint16_t*>(q_out);
+  p->starts = starts;
+  p->inv_freq = inv_freq;
+  p->status = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + kWsStatusOff);
+  p->q_heads = q_heads;
+  p->rotary_dim = rotary_dim;
+  return MARLIN_OK;
+}
+
+static int check_attention(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const int32_t* starts, int tokens,
+                           int q_heads, float scale, int window, void* out, void* workspace, size_t workspace_bytes,
+                           AttentionParams* p) {
+  if (!q || !out) return MARLIN_ERR_NULL;
+  const int st = check_cache(cache, starts, tokens, q_heads, workspace, workspace_bytes, &p->cache);
+  if (st != MARLIN_OK) return st;
+  if (q_heads < 1 || window < 0 || q_stride < 0) return MARLIN_ERR_SHAPE;
+  if (q_stride % 8 || !aligned16(q) || !aligned16(out)) return MARLIN_ERR_ALIGN;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p->q = static_cast<const uint16_t*>(q);
+  p->q_stride = q_stride;
+  p->starts = starts;
+  p->out = static_cast<uint16_t*>(out);
+  p->status = reinterpret_cast<int*>(ws + kWsStatusOff);
+  p->counters = reinterpret_cast<int*>(ws + kWsCounterOff);
+  p->partials = reinterpret_cast<float*>(ws + kWsPartialOff);
+  p->tokens = tokens;
+  p->q_heads = q_heads;
+  p->group = q_heads / cache->kv_heads;
+  p->window = window;
+  p->scale_log2 = scale * 1.44269504088896340736f;
+  return MARLIN_OK;
+}
+
+int marlin_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     void* q_out, const marlin_kv_cache* cache, const int32_t* starts, int tokens, int q_heads,
+                     const float* inv_freq, int rotary_dim, int interleaved, void* workspace, size_t workspace_bytes,
+                     marlin_stream stream) {
+  AppendParams p;
+  int sm_count;
+  int st = check_append(q, q_stride, k, k_stride, v, v_stride, q_out, cache, starts, tokens, q_heads, inv_freq, rotary_dim,
+                        workspace, workspace_bytes, &p);
+  if (st == MARLIN_OK) st = device_is_ours(&sm_count);
+  if (st != MARLIN_OK) return st;
+  return launch_kv_append(p, tokens, interleaved, sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MARLIN_OK
+                                                                                                           : MARLIN_ERR_CUDA;
+}
+
+int marlin_attention_decode(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const int32_t* starts, int tokens,
+                            int q_heads, float scale, int window, void* out, void* workspace, size_t workspace_bytes,
+                            marlin_stream stream) {
+  AttentionParams p;
+  int sm_count;
+  int st = check_attention(q, q_stride, cache, starts, tokens, q_heads, scale, window, out, workspace, workspace_bytes, &p);
+  if (st == MARLIN_OK) st = device_is_ours(&sm_count);
+  if (st != MARLIN_OK) return st;
+  return launch_attention(p, sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MARLIN_OK : MARLIN_ERR_CUDA;
+}
+
+int marlin_attention_block(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o, void* QKV,
+                           void* Q, void* O, void* C, const marlin_kv_cache* cache, const int32_t* starts, int M, int K,
+                           int q_heads, int N, int group_size, const float* inv_freq, int rotary_dim, int interleaved,
+                           float scale, int window, void* workspace, size_t workspace_bytes, marlin_stream stream) {
+  if (!A || !w_qkv || !s_qkv || !w_o || !s_o || !QKV || (inv_freq && !Q) || !O || !C || !cache) return MARLIN_ERR_NULL;
+  const long long head_dim = cache->head_dim, q_cols = q_heads * head_dim, kv_cols = cache->kv_heads * head_dim;
+  const long long columns = q_cols + 2 * kv_cols;
+  if (M < 1 || q_heads < 1 || head_dim < 1 || kv_cols < 1 || columns > 65536 || !shape_ok(K, (int)columns) || !shape_ok((int)q_cols, N))
+    return MARLIN_ERR_SHAPE;
+  if (!normalise_group(K, (int)columns, group_size) || !normalise_group((int)q_cols, N, group_size)) return MARLIN_ERR_GROUP;
+  if (!aligned16(A) || !aligned16(w_qkv) || !aligned16(s_qkv) || !aligned16(w_o) || !aligned16(s_o) || !aligned16(QKV) ||
+      !aligned16(O) || !aligned16(C))
+    return MARLIN_ERR_ALIGN;
+  if (workspace_bytes < workspace_bytes_for(M, K, (int)columns) || workspace_bytes < workspace_bytes_for(M, (int)q_cols, N))
+    return MARLIN_ERR_WORKSPACE;
+  const uint16_t* qkv = static_cast<const uint16_t*>(QKV);
+  const void* q = inv_freq ? Q : QKV;  // without a rotation the queries are read where the layer leaves them
+  const int64_t q_stride = inv_freq ? q_cols : columns;
+  AppendParams append;
+  AttentionParams attention;
+  int sm_count;
+  int st = check_append(inv_freq ? QKV : nullptr, columns, qkv + q_cols, columns, qkv + q_cols + kv_cols, columns,
+                        inv_freq ? Q : nullptr, cache, starts, M, inv_freq ? q_heads : 0, inv_freq, rotary_dim, workspace,
+                        workspace_bytes, &append);
+  if (st == MARLIN_OK)
+    st = check_attention(q, q_stride, cache, starts, M, q_heads, scale, window, O, workspace, workspace_bytes, &attention);
+  if (st == MARLIN_OK) st = device_is_ours(&sm_count);
+  if (st == MARLIN_OK)
+    st = marlin_gemm(A, w_qkv, s_qkv, QKV, M, K, (int)columns, group_size, workspace, workspace_bytes, stream);
+  if (st != MARLIN_OK) return st;
+  if (launch_kv_append(append, M, interleaved, sm_count, static_cast<cudaStream_t>(stream)) != cudaSuccess ||
+      launch_attention(attention, sm_count, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+    return MARLIN_ERR_CUDA;
+  return marlin_gemm(O, w_o, s_o, C, M, (int)q_cols, N, group_size, workspace, workspace_bytes, stream);
 }
 
 int marlin_read_status(const void* workspace, marlin_stream stream) {

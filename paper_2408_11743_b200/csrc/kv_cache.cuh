@@ -1,0 +1,45 @@
+// The paged key-value cache as the kernels see it: tables, positions of new tokens, conversions.  sm_100a only.
+#pragma once
+
+#include "device_utils.cuh"
+#include "marlin_internal.cuh"
+
+namespace marlin_b200 {
+
+// The first report of a call that reaches outside of the cache; a time-out that is already there stays.
+__device__ __forceinline__ void report_cache(int* status) { atomicCAS(status, 0, (int)MARLIN_ERR_CACHE); }
+
+// Length of sequence b, kept inside of what its row of the table can hold.
+__device__ __forceinline__ int cache_length(const KvCacheView& c, int b, int* status) {
+  const int len = __ldg(c.lengths + b);
+  const long long most = (long long)c.max_pages << c.page_shift;
+  if (len < 0 || len > most) {
+    report_cache(status);
+    return len < 0 ? 0 : (int)most;
+  }
+  return len;
+}
+
+// Offset (in elements) of the token at position pos < max_pages * page_size, head h; -1 where its page is not there.
+__device__ __forceinline__ long long cache_offset(const KvCacheView& c, int page, int h, int pos, int* status) {
+  if ((unsigned)page >= (unsigned)c.pages) {
+    report_cache(status);
+    return -1;
+  }
+  return page * c.s_page + h * c.s_head + (pos & ((1 << c.page_shift) - 1)) * c.s_token;
+}
+
+// two fp32 values -> two e4m3 bytes (lo in the lower one): to nearest even, saturating at 448, NaN kept
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// two e4m3 bytes (the lower 16 bits) -> two fp16 values, exact
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return r;
+}
+
+}  // namespace marlin_b200

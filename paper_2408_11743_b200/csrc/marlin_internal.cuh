@@ -118,6 +118,48 @@ cudaError_t launch_permute_zeros(uint8_t* z, uint16_t* zq, int K, int N, int G, 
 // canonical scales [K/G][N] <-> packed order (shared by the dense and the 2:4 pack)
 cudaError_t launch_permute_scales(uint16_t* s, uint16_t* sq, int K, int N, int G, bool inverse, cudaStream_t stream);
 
+// ---- the paged key-value cache (kv_append.cu, attention.cu) --------------------------------------
+struct KvCacheView {
+  void *k, *v;
+  long long s_page, s_head, s_token;  // elements
+  const int* table;
+  long long table_stride;
+  const int* lengths;
+  const float *k_scale, *v_scale;     // 8-bit caches: per key head, or nullptr
+  int pages, max_pages, sequences, kv_heads, head_dim, page_shift;
+  int eight_bit;
+};
+
+struct AppendParams {
+  KvCacheView cache;
+  const uint16_t *q, *k, *v;
+  long long q_stride, k_stride, v_stride;
+  uint16_t* q_out;
+  const int* starts;     // or nullptr: one token per sequence
+  const float* inv_freq; // or nullptr: no rotation
+  int* status;
+  int q_heads, rotary_dim;
+  // filled in by the launch: units of a token, of a query or key head, of those its pairs; units that a thread takes
+  int units, head_units, pair_units, units_per_thread;
+};
+cudaError_t launch_kv_append(AppendParams p, int tokens, int interleaved, int sm_count, cudaStream_t stream);
+
+struct AttentionParams {
+  KvCacheView cache;
+  const uint16_t* q;
+  long long q_stride;
+  const int* starts;     // or nullptr: one token per sequence
+  uint16_t* out;
+  int* status;
+  int* counters;
+  float* partials;
+  int tokens, q_heads, group;  // group: query heads per key head
+  int window;            // 0: none
+  float scale_log2;      // scale * log2(e)
+};
+size_t attention_slot_bytes(int head_dim);
+cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream);
+
 // ---- the stripe partition (host and device use the same two formulas) ------------------------
 // worker w of P owns units [w*U/P, (w+1)*U/P); the owner of unit x is floor(((x+1)*P - 1) / U).
 __host__ __device__ inline long long stripe_begin(long long w, long long U, long long P) { return (w * U) / P; }
