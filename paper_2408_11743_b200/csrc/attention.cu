@@ -6,11 +6,12 @@
 // tiles of 64 keys of (sequence, key head, block of rows), and every CTA takes an equal range of that numbering, whatever
 // the lengths are: the lengths are read on the device, so a captured launch stays balanced as sequences grow.
 //
-// What bounds it: the cache is read once (2 * 2 * head_dim bytes per key and key head), at 16 rows for 4 * 16 * head_dim
-// operations of the tensor cores: 16 operations a byte, so the copies have to be kept in flight and nothing else counts.
+// What bounds it: the cache is read once (2 * 2 * head_dim bytes per key and key head), at 8 rows for 4 * 8 * head_dim
+// operations of the tensor cores: 8 operations a byte, so the copies have to be kept in flight and nothing else counts.
 // Every warp streams keys and values of its own share of a tile through a ring in shared memory (16-byte asynchronous
-// copies, addresses by key, so that a page may end anywhere), and multiplies with mma.sync: up to 64 rows are far below
-// the 128 rows of a tcgen05 tile.
+// copies, addresses by key, so that a page may end anywhere), and multiplies with mma.sync.m16n8k16 with the keys (of S^T = K Q^T)
+// and the values (of O^T = V^T P^T) on the 16-wide side and the rows on the 8-wide one: a decode step has few rows, and
+// eight of them fill an operand.
 #include <limits.h>
 
 #include "kv_cache.cuh"
@@ -18,30 +19,38 @@
 namespace marlin_b200 {
 namespace {
 
-constexpr int kTile = 64;      // keys of a tile
+constexpr int kTile = 64;       // keys of a tile
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kLeastTiles = 2;  // tiles that a CTA takes at least, where there are fewer tiles than CTAs would like
+constexpr uint32_t kMostUnits = 1u << 30;
 constexpr float kNone = -INFINITY;
+// A row's sums are kept relative to 2^base, base its largest logit (in units of log2) when the base was last moved.  It moves only
+// when a logit exceeds it by more than this, so that most tiles neither look for a maximum across lanes nor rescale:
+// weights are then at most 2^8, far from the end of fp16, and their rounding is relative.
+constexpr float kSlack = 8.f;
 
-// DP: head_dim rounded up to 64, 128 or 256.  WM: warps side by side over the rows (16 each); the kWarps / WM teams share
-// out the keys of a tile.  F8: e4m3 cache.
-template <int DP, int WM, bool F8>
+// DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 rows per warp.  TW: warps that share keys and values and have
+// rows of their own (a team); the kWarps / TW teams share out the keys of a tile.  F8: e4m3 cache.
+template <int DP_, int NT, int TW, bool F8>
 struct Geometry {
-  static constexpr int kRows = 16 * WM;
-  static constexpr int kTeams = kWarps / WM;
-  static constexpr int kKeys = kTile / kTeams;       // keys of a tile that a team multiplies
+  static constexpr int DP = DP_;
+  static constexpr int kRows = 8 * NT * TW;
+  static constexpr int kTeams = kWarps / TW;
+  static constexpr int kKeys = 16 * TW;              // keys of a tile that a team multiplies
   static constexpr int kRowBytes = DP * (F8 ? 1 : 2);
   static constexpr int kVectors = kRowBytes / 16;    // 16-byte vectors of a key
   static constexpr int kHalf = kTile * kRowBytes;    // the keys (or the values) of a tile
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kBlocks = DP == 256 ? 1 : 2;  // CTAs per SM
-  static constexpr int kQStride = DP * 2 + 16;       // bytes between rows of Q in shared memory: ldmatrix without conflicts
-  static constexpr int kQBytes = kRows * kQStride;
-  static constexpr int kJoin = kTeams * kRows * (DP + 2) * 4;  // where the teams' sums meet, in the ring
-  static constexpr int kRoom = (kBlocks == 1 ? 220 : 110) * 1024 - kQBytes;
+  static constexpr int kQVectors = DP / 8;
+  static constexpr int kQBytes = kRows * DP * 2;
+  static constexpr int kJoinStride = DP + 4;         // floats between rows of the teams' sums: rows 2 t fall on other banks
+  static constexpr int kJoin = kTeams * kRows * (kJoinStride + 2) * 4;  // where the teams' sums meet, in the ring
+  static constexpr int kRoom = (kBlocks == 1 ? 224 : 112) * 1024 - kQBytes;
   static constexpr int kStages = kRoom / kStage > 8 ? 8 : kRoom / kStage;
   static constexpr int kSmem = kQBytes + kStages * kStage;
+  static constexpr bool kQInRegisters = NT * DP <= 256;
   static_assert(kStages >= 2 && kStages * kStage >= kJoin, "ring");
 };
 
@@ -59,6 +68,12 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t saddr, uint32_t (&r)[
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(saddr));
+}
+// the transpose of an 8 x 8 matrix of 16-bit elements held as the operands hold it
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -78,61 +93,36 @@ __device__ __forceinline__ uint32_t place(int row, int vec) {
   return (uint32_t)(row * VECTORS + v) * 16;
 }
 
-// A row that does not see a key has weight 0 there, and 0 times an infinity or a NaN is NaN.  Keys that no row sees are never
-// loaded; where rows see different keys (several new tokens) such values are left out of the product, and what they stand for
-// is added to the rows that see them: counts of +inf (or NaN) and of -inf (or NaN), by the same MMA on operands of zeros and ones.
-__device__ __forceinline__ bool not_finite(uint32_t two) {
-  return (two & 0x7c00u) == 0x7c00u || (two & 0x7c000000u) == 0x7c000000u;
-}
-struct Operand {
-  uint32_t a[4];
-};
-__device__ __forceinline__ Operand seen_operand(int pos, const int (&low)[2], const int (&high)[2]) {
-  Operand r;
-#pragma unroll
+// A row that does not see a key has weight 0 there, and 0 times an infinity or a NaN is NaN.  Keys that no row of a block sees are
+// never loaded; values of keys that some of its rows see (those around the new tokens, and as many at the edge of a window)
+// are looked through in shared memory, what is not finite is replaced by 0, and added to the rows that see it at the end.
+template <bool F8>
+__device__ __forceinline__ bool clean_vector(uint32_t saddr) {
+  const uint4 v = lds128(saddr);
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool found = false;
   for (int i = 0; i < 4; ++i) {
-    const int row = i & 1, x = pos + (i >> 1) * 8;
-    r.a[i] = (x >= low[row] && x < high[row] ? 0x3c00u : 0u) | (x + 1 >= low[row] && x + 1 < high[row] ? 0x3c000000u : 0u);
-  }
-  return r;
-}
-__device__ __noinline__ float4 add_not_finite_parts(float4 acc, uint4 p, uint4 seen, uint32_t b0, uint32_t b1) {
-  const uint32_t b[2] = {b0, b1};
-  uint32_t finite[2], up[2], down[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    finite[i] = up[i] = down[i] = 0;
-#pragma unroll
-    for (int j = 0; j < 32; j += 16) {
-      const uint32_t x = (b[i] >> j) & 0xffffu, big = x & 0x7fffu;
-      if (big < 0x7c00u) finite[i] |= x << j;
-      if (big > 0x7c00u || x == 0x7c00u) up[i] |= 0x3c00u << j;
-      if (big > 0x7c00u || x == 0xfc00u) down[i] |= 0x3c00u << j;
+    const uint32_t part = F8 ? 0xffu : 0xffffu, most = F8 ? 0x7fu : 0x7c00u;
+    for (int j = 0; j < 32; j += F8 ? 8 : 16) {
+      if (((w[i] >> j) & most) == most) {
+        w[i] &= ~(part << j);
+        found = true;
+      }
     }
   }
-  const uint32_t a[4] = {p.x, p.y, p.z, p.w}, one[4] = {seen.x, seen.y, seen.z, seen.w};
-  float x[4] = {acc.x, acc.y, acc.z, acc.w}, u[4] = {0.f, 0.f, 0.f, 0.f}, d[4] = {0.f, 0.f, 0.f, 0.f};
-  mma_16816(x, a, finite[0], finite[1]);
-  mma_16816(u, one, up[0], up[1]);
-  mma_16816(d, one, down[0], down[1]);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] += (u[i] > 0.f ? INFINITY : 0.f) + (d[i] > 0.f ? -INFINITY : 0.f);
-  return make_float4(x[0], x[1], x[2], x[3]);
-}
-__device__ __forceinline__ void add_not_finite(float (&acc)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const Operand& seen) {
-  const float4 r = add_not_finite_parts(make_float4(acc[0], acc[1], acc[2], acc[3]), make_uint4(a[0], a[1], a[2], a[3]),
-                                        make_uint4(seen.a[0], seen.a[1], seen.a[2], seen.a[3]), b0, b1);
-  acc[0] = r.x; acc[1] = r.y; acc[2] = r.z; acc[3] = r.w;
+  if (found)
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+  return found;
 }
 
-// What a sequence asks for: new tokens [first, first + n) of the call, keys [low, len), tiles [tile0, tile0 + tiles) of
-// them, blocks of rows per key head.  A sequence with new tokens has a tile at least: it writes the zeros.
+// What a sequence asks for: new tokens [first, first + n) of the call, tiles [tile0, tile0 + tiles) of its len keys, blocks of
+// rows per key head.  A sequence with new tokens has a tile at least: it writes the zeros.
 struct Sequence {
-  int len, n, first, low, tile0, tiles, blocks;
+  int len, n, first, tile0, tiles, blocks;
 };
-__device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, int rows, int* status) {
+__device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, int rows) {
   Sequence s;
-  s.len = cache_length(p.cache, b, status);
+  s.len = cache_length(p.cache, b, p.status);
   s.first = b;
   s.n = 1;
   if (p.starts) {
@@ -140,24 +130,42 @@ __device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, in
     s.first = from;
     s.n = to - from;
   }
-  s.low = p.window ? max(0, s.len - s.n - p.window + 1) : 0;
-  s.tile0 = s.low / kTile;
+  s.tile0 = (p.window ? max(0, s.len - s.n - p.window + 1) : 0) / kTile;
   s.tiles = max(1, (s.len + kTile - 1) / kTile - s.tile0);
-  s.blocks = s.n ? (int)(((long long)s.n * p.group + rows - 1) / rows) : 0;
+  s.blocks = (s.n * p.group + rows - 1) / rows;
   return s;
 }
 
-template <int DP, int WM, bool F8>
+// The ranges of the CTAs: worker w of W begins at unit w * (U / W) + min(w, U % W).  A range that would begin within `snap` tiles of
+// the beginning or the end of an item (the tiles of one block of rows) begins there instead: a part of an item costs a
+// round trip through the workspace, which is worth a tile or two where a CTA has few.
+struct Stripes {
+  uint32_t total, workers, size, more, snap;
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * size + min(w, more); }
+  __device__ __forceinline__ uint32_t owner(uint32_t x) const {  // whose range, before any move, holds unit x
+    const uint32_t wide = more * (size + 1);
+    return x < wide ? x / (size + 1) : more + (x - wide) / size;
+  }
+  // boundary x of the ranges where it lies inside of item [i0, i1)
+  __device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t i0, uint32_t i1) const {
+    if (x <= i0 || x >= i1) return x;
+    if (x - i0 <= snap && x - i0 <= i1 - x) return i0;
+    return i1 - x <= snap ? i1 : x;
+  }
+};
+
+template <int DP, int NT, int TW, bool F8>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(const AttentionParams p) {
-  using G = Geometry<DP, WM, F8>;
+  using G = Geometry<DP, NT, TW, F8>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long scan[kWarps];
-  __shared__ long long found_offset;
+  __shared__ uint32_t scan[kWarps];
+  __shared__ uint32_t found_offset;
   __shared__ int found_sequence;
   __shared__ int arrived;
+  __shared__ int not_finite;  // values that were left out of the products of this segment
   const KvCacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int team = warp / WM, wm = warp % WM;
+  const int team = warp / TW, wm = warp % TW;
   const int g = lane >> 2, t4 = lane & 3;
   const uint32_t ring = smem_u32(smem) + G::kQBytes;
   float* const join = reinterpret_cast<float*>(smem + G::kQBytes);
@@ -167,37 +175,47 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
 
   // ---- this CTA's range of tiles: thread i counts the tiles of sequences [i * per, (i + 1) * per)
   const int per = (c.sequences + kThreads - 1) / kThreads;
-  long long mine = 0;
+  uint32_t mine = 0;
   for (int b = tid * per; b < min(c.sequences, (tid + 1) * per); ++b) {
-    const Sequence s = sequence(p, b, G::kRows, p.status);
-    mine += (long long)c.kv_heads * s.blocks * s.tiles;
+    const Sequence s = sequence(p, b, G::kRows);
+    const unsigned long long units = (unsigned long long)c.kv_heads * s.blocks * s.tiles + mine;
+    mine = (uint32_t)min(units, (unsigned long long)kMostUnits);
   }
-  long long before = mine;
+  uint32_t before = mine;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
-    const long long x = __shfl_up_sync(~0u, before, d);
-    if (lane >= d) before += x;
+    const uint32_t x = __shfl_up_sync(~0u, before, d);
+    if (lane >= d) before = min(before + x, kMostUnits);
   }
   if (lane == 31) scan[warp] = before;
+  if (tid == 0) not_finite = 0;
   __syncthreads();
-  long long total = 0;
+  Stripes stripes;
+  stripes.total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
+    if (w < warp) before = min(before + scan[w], kMostUnits);
+    stripes.total = min(stripes.total + scan[w], kMostUnits);
+  }
+  if (stripes.total == kMostUnits) {  // more tiles than are numbered (2^30: weeks of work): refused
+    report_cache(p.status);
+    return;
   }
   before -= mine;
-  const long long workers = min((long long)gridDim.x, max(1ll, total / kLeastTiles));
-  if (blockIdx.x >= workers) return;
-  long long at = stripe_begin(blockIdx.x, total, workers);
-  const long long end = stripe_begin(blockIdx.x + 1, total, workers);
+  stripes.workers = min(gridDim.x, max(1u, stripes.total / kLeastTiles));
+  if (blockIdx.x >= stripes.workers) return;
+  stripes.size = stripes.total / stripes.workers;
+  stripes.more = stripes.total % stripes.workers;
+  stripes.snap = stripes.size < 8 ? 2 : 0;
+  uint32_t at = stripes.begin(blockIdx.x);
+  const uint32_t end = stripes.begin(blockIdx.x + 1);
   if (at >= end) return;  // (nothing to do at all)
   if (mine > 0 && before <= at && at < before + mine) {
     int b = tid * per;
-    long long off = at - before;
+    uint32_t off = at - before;
     for (;; ++b) {
-      const Sequence s = sequence(p, b, G::kRows, p.status);
-      const long long units = (long long)c.kv_heads * s.blocks * s.tiles;
+      const Sequence s = sequence(p, b, G::kRows);
+      const uint32_t units = (uint32_t)c.kv_heads * s.blocks * s.tiles;
       if (off < units) break;
       off -= units;
     }
@@ -206,53 +224,98 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
   }
   __syncthreads();
   int b = found_sequence;
-  long long off = found_offset;
-  Sequence s = sequence(p, b, G::kRows, p.status);
+  uint32_t off = found_offset;
+  Sequence s = sequence(p, b, G::kRows);
+  uint32_t item = off / (uint32_t)s.tiles;     // (key head, block of rows) of the sequence
+  uint32_t skip = off - item * (uint32_t)s.tiles;
+  {
+    const uint32_t i0 = at - skip, to = stripes.moved(at, i0, i0 + s.tiles);
+    skip += to - at;
+    at = to;
+  }
 
-  while (at < end) {
+#pragma unroll 1
+  for (;;) {
+    if (skip == (uint32_t)s.tiles) {  // the next item
+      if (at >= end) return;
+      skip = 0;
+      if (++item == (uint32_t)(c.kv_heads * s.blocks)) {
+        item = 0;
+        do s = sequence(p, ++b, G::kRows);
+        while (s.blocks == 0);
+      }
+    }
     // ---- one segment: tiles [tile, tile + nt) of (sequence b, key head h, block of rows rb)
-    const int item = (int)(off / s.tiles), skip = (int)(off % s.tiles);
-    const int h = item / s.blocks, rb = item % s.blocks;
-    const int tile = s.tile0 + skip;
-    const int nt = (int)min((long long)(s.tiles - skip), end - at);
-    const int rows = (int)min((long long)G::kRows, (long long)s.n * p.group - (long long)rb * G::kRows);
+    const uint32_t i0 = at - skip, i1 = i0 + s.tiles;
+    const uint32_t to = min(stripes.moved(end, i0, i1), i1);
+    if (at >= to) return;
+    const int nt = (int)(to - at);
+    const int h = (int)(item / (uint32_t)s.blocks), rb = (int)item - h * s.blocks;
+    const int tile = s.tile0 + (int)skip;
     const int row0 = rb * G::kRows;  // row r is query head h * group + r % group of new token r / group
+    const int rows = min(G::kRows, s.n * p.group - row0);
+    // row r sees the positions [high - window, high) (all below high without a window), high = base_high + its token; the block
+    // as a whole [low_min, high_max), and all of its rows [low_max, high_min)
+    const int base_high = s.len - s.n + 1;
+    const int token_first = row0 / p.group, token_last = (row0 + rows - 1) / p.group;
+    const int high_min = base_high + token_first, high_max = base_high + token_last;
+    const int low_min = p.window ? max(0, high_min - p.window) : 0, low_max = p.window ? max(0, high_max - p.window) : 0;
 
     // ---- copies: every warp brings 16 keys and values of a tile, in most layouts just those that it multiplies
-    auto page_of = [&](int step) {  // lanes 0 - 15: the page of the warp's key, or -1
+    constexpr int kPer = G::kVectors < 32 ? 32 / G::kVectors : 1;  // keys per pass of the warp
+    constexpr int kElement = F8 ? 1 : 2;
+    const int my_row = lane / G::kVectors, my_vec = lane % G::kVectors;
+    const bool my_part = my_vec * (16 / kElement) < c.head_dim;
+    const long long step_bytes = c.s_token * kElement;
+    const long long my_bytes = my_row * step_bytes + my_vec * 16;
+    const int* const table = c.table + b * c.table_stride;
+    auto page_of = [&](int step) {  // the page of key lane % 16 of the warp's sixteen, -1 where it is not asked for
       const int key = (tile + step) * kTile + warp * 16 + (lane & 15);
-      return step < nt && key >= s.low && key < s.len ? __ldg(c.table + b * c.table_stride + (key >> c.page_shift)) : -2;
+      return step < nt && key >= low_min && key < high_max ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
     };
     auto bring = [&](int step, int page) {
       if (step < nt) {
-        const int key = (tile + step) * kTile + warp * 16 + (lane & 15);
-        const long long mine = page == -2 ? -1 : cache_offset(c, page, h, key, p.status);
+        const int key0 = (tile + step) * kTile + warp * 16;
         const uint32_t stage = ring + (step % G::kStages) * G::kStage;
-        constexpr int kPer = G::kVectors < 32 ? 32 / G::kVectors : 1;  // keys per pass of the warp
+        const long long off = page == INT_MIN ? -1 : cache_offset(c, page, h, key0 + (lane & 15), p.status);
+        const bool one_page = c.page_shift >= 4 && __all_sync(~0u, off >= 0);
+        if (one_page) {  // sixteen keys of one page: their places are s_token apart
+          const long long first = __shfl_sync(~0u, off, 0) * kElement + my_bytes;
+          const uint8_t* k = static_cast<const uint8_t*>(c.k) + first;
+          const uint8_t* v = static_cast<const uint8_t*>(c.v) + first;
 #pragma unroll
-        for (int r = 0; r < 16; r += kPer) {
-          const int row = r + lane / G::kVectors, vec = lane % G::kVectors;
-          const long long from = __shfl_sync(~0u, mine, row);
-          const bool there = from >= 0 && vec * (F8 ? 16 : 8) < c.head_dim;
-          const long long bytes = there ? (from * (F8 ? 1 : 2) + vec * 16) : 0;
-          const uint32_t to = stage + place<G::kVectors>(warp * 16 + row, vec);
-          copy16(to, static_cast<const uint8_t*>(c.k) + bytes, there);
-          copy16(to + G::kHalf, static_cast<const uint8_t*>(c.v) + bytes, there);
+          for (int r = 0; r < 16; r += kPer) {
+            const uint32_t dst = stage + place<G::kVectors>(warp * 16 + r + my_row, my_vec);
+            copy16(dst, my_part ? k : c.k, my_part);
+            copy16(dst + G::kHalf, my_part ? v : c.v, my_part);
+            k += kPer * step_bytes;
+            v += kPer * step_bytes;
+          }
+        } else {
+#pragma unroll 1
+          for (int r = 0; r < 16; r += kPer) {
+            const long long from = __shfl_sync(~0u, off, r + my_row);
+            const bool there = from >= 0 && my_part;
+            const long long bytes = there ? from * kElement + my_vec * 16 : 0;
+            const uint32_t dst = stage + place<G::kVectors>(warp * 16 + r + my_row, my_vec);
+            copy16(dst, static_cast<const uint8_t*>(c.k) + bytes, there);
+            copy16(dst + G::kHalf, static_cast<const uint8_t*>(c.v) + bytes, there);
+          }
         }
       }
       copies_commit();
     };
+    int page = page_of(0);
 
     // Q goes with the first tile; rows and elements that are not there are zeros
-    constexpr int kQVectors = DP / 8;
-    for (int i = tid; i < G::kRows * kQVectors; i += kThreads) {
-      const int r = i / kQVectors, vec = i % kQVectors;
-      const int token = (row0 + r) / p.group, head = h * p.group + (row0 + r) % p.group;
+#pragma unroll 1
+    for (int i = tid; i < G::kRows * G::kQVectors; i += kThreads) {
+      const int r = i / G::kQVectors, vec = i % G::kQVectors;
+      const int token = (row0 + r) / p.group, head = h * p.group + (row0 + r) - token * p.group;
       const bool there = r < rows && vec * 8 < c.head_dim;
       const uint16_t* src = p.q + (there ? (long long)(s.first + token) * p.q_stride + head * c.head_dim + vec * 8 : 0);
-      copy16(smem_u32(smem) + r * G::kQStride + vec * 16, src, there);
+      copy16(smem_u32(smem) + place<G::kQVectors>(r, vec), src, there);
     }
-    int page = page_of(0);
 #pragma unroll 1
     for (int i = 0; i < G::kStages - 1; ++i) {
       const int next = page_of(i + 1);
@@ -260,211 +323,290 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
       page = next;
     }
 
-    // the positions that the rows of this thread see: [low, high)
-    int high[2], low[2];
+    // positions below which the rows of this thread see (rows that are not there: as the last one)
+    int high[NT][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = wm * 16 + g + 8 * i;
-      const int pos = s.len - s.n + (row0 + r) / p.group;
-      high[i] = r < rows ? pos + 1 : INT_MAX;  // (rows that are not there: Q is zero, the results are not used)
-      low[i] = r < rows && p.window ? max(0, pos - p.window + 1) : 0;
-    }
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) high[j][i] = base_high + (row0 + min(rows - 1, wm * 8 * NT + j * 8 + t4 * 2 + i)) / p.group;
     const float factor = p.scale_log2 * (F8 && c.k_scale ? __ldg(c.k_scale + h) : 1.f);
 
-    constexpr bool kQInRegisters = DP <= 128;
-    uint32_t q[kQInRegisters ? DP / 16 : 1][4];
-    float m[2] = {kNone, kNone}, l[2] = {0.f, 0.f};
-    float o[DP / 8][4];
+    // operands of Q: rows on the 8-wide side; of 16 elements a thread has 2 t, 2 t + 1, 2 t + 8, 2 t + 9, or, to match the
+    // bytes of an 8-bit key, 4 t .. 4 t + 3
+    const uint32_t q_base = smem_u32(smem);
+    const int q_row = wm * 8 * NT;
+    uint32_t q[G::kQInRegisters ? DP / 16 : 1][NT][2];
+    auto load_q = [&](int ks, uint32_t (&x)[NT][2]) {
 #pragma unroll
-    for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-
-    auto load_q = [&](int ks, uint32_t (&a)[4]) {
-      const uint32_t base = smem_u32(smem) + (wm * 16) * G::kQStride;
-      if (F8) {  // the order of the elements within 16 is that of the keys' bytes: 4 t .. 4 t + 3 in a thread
-        const uint2 x = lds64(base + g * G::kQStride + ks * 32 + t4 * 8);
-        const uint2 y = lds64(base + (g + 8) * G::kQStride + ks * 32 + t4 * 8);
-        a[0] = x.x; a[1] = y.x; a[2] = x.y; a[3] = y.y;
-      } else {
-        ldmatrix_x4(base + (lane & 15) * G::kQStride + ks * 32 + (lane >> 4) * 16, a);
+      for (int j = 0; j < NT; ++j) {
+        if (F8) {
+          const uint2 y = lds64(q_base + place<G::kQVectors>(q_row + j * 8 + g, 2 * ks + (t4 >> 1)) + (t4 & 1) * 8);
+          x[j][0] = y.x;
+          x[j][1] = y.y;
+        } else if (NT % 2 == 0) {
+          if (j % 2 == 0) {
+            uint32_t y[4];
+            ldmatrix_x4(q_base + place<G::kQVectors>(q_row + j * 8 + (lane & 7) + (lane >> 4) * 8, 2 * ks + ((lane >> 3) & 1)), y);
+            x[j][0] = y[0];
+            x[j][1] = y[1];
+            x[NT % 2 == 0 ? j + 1 : 0][0] = y[2];
+            x[NT % 2 == 0 ? j + 1 : 0][1] = y[3];
+          }
+        } else {
+          x[j][0] = lds32(q_base + place<G::kQVectors>(q_row + j * 8 + g, 2 * ks) + t4 * 4);
+          x[j][1] = lds32(q_base + place<G::kQVectors>(q_row + j * 8 + g, 2 * ks + 1) + t4 * 4);
+        }
       }
     };
+
+    float m[NT][2], l[NT][2];
+    float o[DP / 16][NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      m[j][0] = m[j][1] = kNone;
+      l[j][0] = l[j][1] = 0.f;
+#pragma unroll
+      for (int v = 0; v < DP / 16; ++v) o[v][j][0] = o[v][j][1] = o[v][j][2] = o[v][j][3] = 0.f;
+    }
+    bool open = true;  // some row has not seen a key yet
 
 #pragma unroll 1
     for (int step = 0; step < nt; ++step) {
       copies_wait<G::kStages - 2>();
-      if (WM == 1 && step > 0) __syncwarp(); else __syncthreads();  // (the first time for Q)
+      if (step == 0 || TW == kWarps)
+        __syncthreads();  // (the first time for Q)
+      else if (TW == 1)
+        __syncwarp();
+      else
+        named_bar_sync(1 + team, 32 * TW);
       {
         const int next = page_of(step + G::kStages);
         bring(step + G::kStages - 1, page);
         page = next;
       }
-      if (kQInRegisters && step == 0) {
+      if (G::kQInRegisters && step == 0) {
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) load_q(ks, q[kQInRegisters ? ks : 0]);
+        for (int ks = 0; ks < DP / 16; ++ks) load_q(ks, q[G::kQInRegisters ? ks : 0]);
       }
       const uint32_t keys = ring + (step % G::kStages) * G::kStage, values = keys + G::kHalf;
       const int key0 = team * G::kKeys;
 
-      // S = Q K^T
-      float sc[G::kKeys / 8][4];
+      // S^T = K Q^T: a thread has keys g, g + 8 of 16 and rows 2 t, 2 t + 1 of 8.  (One tile alone would be a chain of dependent
+      // products: it is summed in two.)
+      constexpr int kChains = NT * TW == 1 ? 2 : 1;
+      float x[TW][NT][kChains][4];
 #pragma unroll
-      for (int i = 0; i < G::kKeys / 8; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+      for (int kk = 0; kk < TW; ++kk)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < kChains; ++i) x[kk][j][i][0] = x[kk][j][i][1] = x[kk][j][i][2] = x[kk][j][i][3] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < DP / 16; ks += F8 ? 2 : 1) {
-        uint32_t a[F8 ? 2 : 1][4];
-#pragma unroll
-        for (int i = 0; i < (F8 ? 2 : 1); ++i) {
-          if (kQInRegisters) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) a[i][j] = q[kQInRegisters ? ks + i : 0][j];
-          } else {
-            load_q(ks + i, a[i]);
-          }
+        uint32_t qs[F8 ? 2 : 1][NT][2];
+        if (!G::kQInRegisters) {
+          load_q(ks, qs[0]);
+          if (F8) load_q(ks + 1, qs[F8 ? 1 : 0]);
         }
 #pragma unroll
-        for (int kk = 0; kk < G::kKeys / 16; ++kk) {
+        for (int kk = 0; kk < TW; ++kk) {
           uint32_t r[4];
-          if (F8) {
-            const int row = key0 + kk * 16 + (lane & 15);
-            ldmatrix_x4(keys + place<G::kVectors>(row, ks + (lane >> 4)), r);
+          ldmatrix_x4(keys + place<G::kVectors>(key0 + kk * 16 + (lane & 15), (F8 ? ks : 2 * ks) + (lane >> 4)), r);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {  // r[2 i]: keys 0 - 7, r[2 i + 1]: keys 8 - 15 of 16 elements
-              mma_16816(sc[2 * kk], a[F8 ? i : 0], e4m3x2_to_f16x2(r[2 * i]), e4m3x2_to_f16x2(r[2 * i] >> 16));
-              mma_16816(sc[2 * kk + 1], a[F8 ? i : 0], e4m3x2_to_f16x2(r[2 * i + 1]), e4m3x2_to_f16x2(r[2 * i + 1] >> 16));
+          for (int i = 0; i < (F8 ? 2 : 1); ++i) {
+            uint32_t a[4];
+            if (F8) {  // r[2 i]: keys 0 - 7, r[2 i + 1]: keys 8 - 15 of 16 elements
+              a[0] = e4m3x2_to_f16x2(r[F8 ? 2 * i : 0]);
+              a[1] = e4m3x2_to_f16x2(r[F8 ? 2 * i + 1 : 0]);
+              a[2] = e4m3x2_to_f16x2(r[F8 ? 2 * i : 0] >> 16);
+              a[3] = e4m3x2_to_f16x2(r[F8 ? 2 * i + 1 : 0] >> 16);
+            } else {
+              a[0] = r[0]; a[1] = r[1]; a[2] = r[2]; a[3] = r[3];
             }
-          } else {
-            const int row = key0 + kk * 16 + (lane & 7) + (lane >> 4) * 8;
-            ldmatrix_x4(keys + place<G::kVectors>(row, 2 * ks + ((lane >> 3) & 1)), r);
-            mma_16816(sc[2 * kk], a[0], r[0], r[1]);
-            mma_16816(sc[2 * kk + 1], a[0], r[2], r[3]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              const uint32_t(&y)[2] = G::kQInRegisters ? q[G::kQInRegisters ? ks + i : 0][j] : qs[F8 ? i : 0][j];
+              mma_16816(x[kk][j][(F8 ? i : ks) % kChains], a, y[0], y[1]);
+            }
           }
         }
       }
 
-      // softmax of this tile: logits in units of log2, -inf where a row does not see the key
+      // logits in units of log2, relative to the base; -inf where a row does not see the key
       const int pos0 = (tile + step) * kTile + key0;
-      const bool all = pos0 >= max(low[0], low[1]) && pos0 + G::kKeys <= min(high[0], high[1]);
-      float top[2] = {kNone, kNone};
+      const bool all = pos0 >= low_max && pos0 + G::kKeys <= high_min;  // (the same for the team)
+      bool over = open;
 #pragma unroll
-      for (int i = 0; i < G::kKeys / 8; ++i) {
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int pos = pos0 + i * 8 + t4 * 2 + (j & 1);
-          const bool seen = all || (pos >= low[j >> 1] && pos < high[j >> 1]);
-          sc[i][j] = seen ? sc[i][j] * factor : kNone;
-          top[j >> 1] = fmaxf(top[j >> 1], sc[i][j]);
-        }
-      }
-      float alpha[2], base[2];
+        for (int i = 0; i < 2; ++i) {
+          const float base = m[j][i] == kNone ? 0.f : m[j][i];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 1));
-        top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 2));
-        const float now = fmaxf(m[i], top[i]);
-        base[i] = now == kNone ? 0.f : now;
-        alpha[i] = exp2_fast(m[i] - base[i]);
-        m[i] = now;
-        l[i] *= alpha[i];
-      }
-      if (__any_sync(~0u, alpha[0] != 1.f || alpha[1] != 1.f)) {
+          for (int kk = 0; kk < TW; ++kk)
 #pragma unroll
-        for (int i = 0; i < DP / 8; ++i) {
-          o[i][0] *= alpha[0]; o[i][1] *= alpha[0];
-          o[i][2] *= alpha[1]; o[i][3] *= alpha[1];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < G::kKeys / 8; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sc[i][j] = exp2_fast(sc[i][j] - base[j >> 1]);
-          l[j >> 1] += sc[i][j];
-        }
-      }
-
-      const bool differ = s.n > 1 && __any_sync(~0u, !all);
-
-      // O += P V, P rounded to fp16 (weights of at most 1: off by 2^-12 of the largest, 2^-25 at the least)
-#pragma unroll
-      for (int kk = 0; kk < G::kKeys / 16; ++kk) {
-        const uint32_t a[4] = {half2_bits(sc[2 * kk][0], sc[2 * kk][1]), half2_bits(sc[2 * kk][2], sc[2 * kk][3]),
-                               half2_bits(sc[2 * kk + 1][0], sc[2 * kk + 1][1]), half2_bits(sc[2 * kk + 1][2], sc[2 * kk + 1][3])};
-        const int row = key0 + kk * 16 + (lane & 15);
-#pragma unroll
-        for (int v = 0; v < G::kVectors; v += 2) {
-          uint32_t r[4];
-          ldmatrix_x4_trans(values + place<G::kVectors>(row, v + (lane >> 4)), r);
-          uint32_t bv[F8 ? 4 : 2][2];  // operands of the n-tiles
-          if (F8) {
-            // r[2 i], r[2 i + 1] of vector v + i: bytes (key 2 t: elements 2 g, 2 g + 1), (key 2 t + 1: the same), keys + 8 in
-            // the second; the n-tiles take the even and the odd elements of the 16
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t x = __byte_perm(r[i], 0, 0x3120);
-              bv[(i >> 1) * 2 + 0][i & 1] = e4m3x2_to_f16x2(x);
-              bv[F8 ? (i >> 1) * 2 + 1 : 0][i & 1] = e4m3x2_to_f16x2(x >> 16);
+            for (int e = i; e < 4; e += 2) {
+              float& y = x[kk][j][0][e];
+              if (kChains == 2) y += x[kk][j][kChains - 1][e];
+              y = fmaf(y, factor, -base);
+              over |= y > kSlack;
             }
+        }
+      if (!all) {
+#pragma unroll
+        for (int kk = 0; kk < TW; ++kk)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int pos = pos0 + kk * 16 + g + (e >> 1) * 8;
+              const bool seen = pos < high[j][e & 1] && (p.window == 0 || pos >= high[j][e & 1] - p.window);
+              if (!seen) x[kk][j][0][e] = kNone;
+            }
+      }
+      if (__any_sync(~0u, over)) {  // move the bases
+        bool none = false;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float top = kNone;
+#pragma unroll
+            for (int kk = 0; kk < TW; ++kk) top = fmaxf(top, fmaxf(x[kk][j][0][i], x[kk][j][0][i + 2]));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+            const float old = m[j][i] == kNone ? 0.f : m[j][i];
+            const float now = fmaxf(m[j][i], top + old);
+            const float base = now == kNone ? 0.f : now;
+            const float alpha = exp2_fast(m[j][i] - base), shift = old - base;
+            m[j][i] = now;
+            none |= now == kNone;
+            l[j][i] *= alpha;
+#pragma unroll
+            for (int kk = 0; kk < TW; ++kk) {
+              x[kk][j][0][i] += shift;
+              x[kk][j][0][i + 2] += shift;
+            }
+#pragma unroll
+            for (int v = 0; v < DP / 16; ++v) {
+              o[v][j][i] *= alpha;
+              o[v][j][i + 2] *= alpha;
+            }
+          }
+        open = __any_sync(~0u, none);
+      }
+
+      // weights, rounded to fp16 for the product (2^-12 of each on average, or 2^-25 of the largest), and turned round: keys on the
+      // side that is summed over
+      uint32_t w[TW][NT][2];
+#pragma unroll
+      for (int kk = 0; kk < TW; ++kk)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          float (&y)[4] = x[kk][j][0];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y[e] = exp2_fast(y[e]);
+            l[j][e & 1] += y[e];
+          }
+          w[kk][j][0] = transpose8x8(half2_bits(y[0], y[1]));
+          w[kk][j][1] = transpose8x8(half2_bits(y[2], y[3]));
+        }
+
+      if (s.n > 1 && !all) {  // values of keys that not every row sees
+        bool found = false;
+#pragma unroll 1
+        for (int i = lane + 32 * wm; i < G::kKeys * G::kVectors; i += 32 * TW) {
+          const int row = key0 + i / G::kVectors, pos = (tile + step) * kTile + row;
+          if ((pos >= high_min && pos < high_max) || (pos >= low_min && pos < low_max))
+            found |= clean_vector<F8>(values + place<G::kVectors>(row, i % G::kVectors));
+        }
+        if (found) not_finite = 1;
+        if (TW == 1) __syncwarp(); else named_bar_sync(1 + team, 32 * TW);
+      }
+
+      // O^T += V^T P^T: a thread has elements g, g + 8 (8-bit: 2 g, 2 g + 1) of 16 and rows 2 t, 2 t + 1 of 8
+#pragma unroll
+      for (int v = 0; v < DP / 16; v += F8 ? 2 : 1) {
+#pragma unroll
+        for (int kk = 0; kk < TW; ++kk) {
+          uint32_t r[4];
+          if (F8) {
+            // r[2 i], r[2 i + 1] of vector v + i: bytes (key 2 t: elements 2 g, 2 g + 1), (key 2 t + 1: the same); keys + 8
+            ldmatrix_x4_trans(values + place<G::kVectors>(key0 + kk * 16 + (lane & 15), v + (lane >> 4)), r);
           } else {
-            bv[0][0] = r[0]; bv[0][1] = r[1]; bv[1][0] = r[2]; bv[1][1] = r[3];
+            ldmatrix_x4_trans(values + place<G::kVectors>(key0 + kk * 16 + (lane & 7) + (lane >> 4) * 8, 2 * v + ((lane >> 3) & 1)), r);
           }
 #pragma unroll
-          for (int i = 0; i < (F8 ? 4 : 2); ++i) {
-            float (&acc)[4] = o[(F8 ? 2 * v : v) + i];
-            if (differ && __any_sync(~0u, not_finite(bv[i][0]) || not_finite(bv[i][1])))
-              add_not_finite(acc, a, bv[i][0], bv[i][1], seen_operand(pos0 + kk * 16 + t4 * 2, low, high));
-            else
-              mma_16816(acc, a, bv[i][0], bv[i][1]);
+          for (int i = 0; i < (F8 ? 2 : 1); ++i) {
+            uint32_t a[4];
+            if (F8) {
+              const uint32_t y = __byte_perm(r[F8 ? 2 * i : 0], 0, 0x3120), z = __byte_perm(r[F8 ? 2 * i + 1 : 0], 0, 0x3120);
+              a[0] = e4m3x2_to_f16x2(y);
+              a[1] = e4m3x2_to_f16x2(y >> 16);
+              a[2] = e4m3x2_to_f16x2(z);
+              a[3] = e4m3x2_to_f16x2(z >> 16);
+            } else {
+              a[0] = r[0]; a[1] = r[1]; a[2] = r[2]; a[3] = r[3];
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) mma_16816(o[F8 ? v + i : v][j], a, w[kk][j][0], w[kk][j][1]);
           }
         }
       }
     }
 
-    // ---- the teams' sums meet: [team][row][DP] in the ring, with m and l behind
+    // ---- the teams' sums meet: [team][row] in the ring, with m and l behind
     copies_wait<0>();
     __syncthreads();
-    constexpr int kTeamFloats = G::kRows * DP;
+    constexpr int kTeamFloats = G::kRows * G::kJoinStride;
     float* const ml = join + G::kTeams * kTeamFloats;  // [team][row][2]
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      l[i] += __shfl_xor_sync(~0u, l[i], 1);
-      l[i] += __shfl_xor_sync(~0u, l[i], 2);
-      const int r = wm * 16 + g + 8 * i;
-      if (r < rows) {
-        if (t4 == 0) {
-          ml[(team * G::kRows + r) * 2] = m[i];
-          ml[(team * G::kRows + r) * 2 + 1] = l[i];
-        }
-        float* dst = join + team * kTeamFloats + r * DP;
-        if (F8) {
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int v = 0; v < DP / 16; ++v)
-            *reinterpret_cast<float4*>(dst + v * 16 + t4 * 4) =
-                make_float4(o[2 * v][2 * i], o[2 * v + 1][2 * i], o[2 * v][2 * i + 1], o[2 * v + 1][2 * i + 1]);
-        } else {
+      for (int i = 0; i < 2; ++i) {
+        l[j][i] += __shfl_xor_sync(~0u, l[j][i], 4);
+        l[j][i] += __shfl_xor_sync(~0u, l[j][i], 8);
+        l[j][i] += __shfl_xor_sync(~0u, l[j][i], 16);
+        const int r = wm * 8 * NT + j * 8 + t4 * 2 + i;
+        if (r < rows) {
+          if (g == 0) {
+            ml[(team * G::kRows + r) * 2] = m[j][i];
+            ml[(team * G::kRows + r) * 2 + 1] = l[j][i];
+          }
+          float* dst = join + team * kTeamFloats + r * G::kJoinStride;
 #pragma unroll
-          for (int v = 0; v < DP / 8; ++v)
-            *reinterpret_cast<float2*>(dst + v * 8 + t4 * 2) = make_float2(o[v][2 * i], o[v][2 * i + 1]);
+          for (int v = 0; v < DP / 16; ++v) {
+            dst[v * 16 + (F8 ? 2 * g : g)] = o[v][j][i];
+            dst[v * 16 + (F8 ? 2 * g + 1 : g + 8)] = o[v][j][i + 2];
+          }
         }
       }
-    }
     __syncthreads();
 
     // who else has tiles of this item: CTAs c0 .. c1; c0 leaves its part in the second slot of its two, the others in the first
-    const long long item0 = at - skip;
-    const int c0 = stripe_owner(item0, total, workers), c1 = stripe_owner(item0 + s.tiles - 1, total, workers);
-    const bool whole = c0 == c1;
+    uint32_t c0 = blockIdx.x, c1 = blockIdx.x;
+    const bool whole = nt == s.tiles;
+    if (!whole) {
+      c0 = stripes.owner(i0);
+      while (c0 + 1 < stripes.workers && stripes.begin(c0 + 1) < i1 && stripes.moved(stripes.begin(c0 + 1), i0, i1) == i0) ++c0;
+      c1 = stripes.owner(i1 - 1);
+      while (stripes.begin(c1) > i0 && stripes.moved(stripes.begin(c1), i0, i1) == i1) --c1;
+    }
     constexpr int kSlot = G::kRows * (DP + 2);
-    auto slot = [&](int cta) { return p.partials + (size_t)(2 * cta + (cta == c0)) * kSlot; };
+    auto slot = [&](uint32_t cta) { return p.partials + (size_t)(2 * cta + (cta == c0)) * kSlot; };
     auto write_out = [&](int r, int d, float4 x, float li) {
-      const int token = (row0 + r) / p.group, head = h * p.group + (row0 + r) % p.group;
-      const int pos = s.len - s.n + token;
-      const float f = pos < 0 ? 0.f : (F8 && c.v_scale ? __ldg(c.v_scale + h) : 1.f) / li;
-      if (pos < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int token = (row0 + r) / p.group, head = h * p.group + (row0 + r) - token * p.group;
+      const bool nothing = base_high + token <= 0;
+      const float f = nothing ? 0.f : (F8 && c.v_scale ? __ldg(c.v_scale + h) : 1.f) / li;
+      if (nothing) x = make_float4(0.f, 0.f, 0.f, 0.f);
       uint2 w;
       w.x = half2_bits(x.x * f, x.y * f);
       w.y = half2_bits(x.z * f, x.w * f);
       *reinterpret_cast<uint2*>(p.out + ((long long)(s.first + token) * p.q_heads + head) * c.head_dim + d) = w;
     };
+    const bool odd_values = s.n > 1 && not_finite;
+#pragma unroll 1
     for (int i = tid; i < rows * (DP / 4); i += kThreads) {
       const int r = i / (DP / 4), d = (i % (DP / 4)) * 4;
       if (d >= c.head_dim) continue;
@@ -477,9 +619,32 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
 #pragma unroll
       for (int w = 0; w < G::kTeams; ++w) {
         const float f = exp2_fast(ml[(w * G::kRows + r) * 2] - base);
-        const float4 y = *reinterpret_cast<const float4*>(join + w * kTeamFloats + r * DP + d);
+        const float4 y = *reinterpret_cast<const float4*>(join + w * kTeamFloats + r * G::kJoinStride + d);
         li += ml[(w * G::kRows + r) * 2 + 1] * f;
         x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+      }
+      if (odd_values) {
+        const int high = base_high + (row0 + r) / p.group, low = p.window ? max(0, high - p.window) : 0;
+#pragma unroll 1
+        for (int pos = max(low, tile * kTile); pos < min(high, (tile + nt) * kTile); ++pos) {
+          if (pos >= low_max && pos < high_min) {  // (every row sees these: they were left where they are)
+            pos = high_min - 1;
+            continue;
+          }
+          const long long off = cache_offset(c, __ldg(table + (pos >> c.page_shift)), h, pos, p.status);
+          if (off < 0) continue;
+          float v[4];
+          for (int e = 0; e < 4; ++e) {
+            if (F8) {
+              const uint32_t y = e4m3x2_to_f16x2(static_cast<const uint8_t*>(c.v)[off + d + e]);
+              v[e] = __low2float(*reinterpret_cast<const __half2*>(&y));
+            } else {
+              v[e] = __half2float(static_cast<const __half*>(c.v)[off + d + e]);
+            }
+            if (isfinite(v[e])) v[e] = 0.f;
+          }
+          x.x += v[0]; x.y += v[1]; x.z += v[2]; x.w += v[3];
+        }
       }
       if (whole) {
         write_out(r, d, x, li);
@@ -497,18 +662,19 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
       __syncthreads();
       if (tid == 0) arrived = atom_add_acq_rel_gpu(p.counters + c0, 1);
       __syncthreads();
-      if (arrived == c1 - c0) {  // the last one: every part is there
+      if (arrived == (int)(c1 - c0)) {  // the last one: every part is there
         __threadfence();
         if (tid == 0) p.counters[c0] = 0;
+#pragma unroll 1
         for (int i = tid; i < rows * (DP / 4); i += kThreads) {
           const int r = i / (DP / 4), d = (i % (DP / 4)) * 4;
           if (d >= c.head_dim) continue;
           float mi = kNone;
-          for (int w = c0; w <= c1; ++w) mi = fmaxf(mi, __ldcg(slot(w) + G::kRows * DP + 2 * r));
+          for (uint32_t w = c0; w <= c1; ++w) mi = fmaxf(mi, __ldcg(slot(w) + G::kRows * DP + 2 * r));
           const float base = mi == kNone ? 0.f : mi;
           float li = 0.f;
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int w = c0; w <= c1; ++w) {
+          for (uint32_t w = c0; w <= c1; ++w) {
             const float* from = slot(w);
             const float2 part = __ldcg(reinterpret_cast<const float2*>(from + G::kRows * DP + 2 * r));
             const float f = exp2_fast(part.x - base);
@@ -520,22 +686,18 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
         }
       }
     }
+    if (tid == 0) not_finite = 0;
     __syncthreads();  // the ring and Q are free again
-
-    at += nt;
-    off += nt;
-    if (at < end && off == (long long)c.kv_heads * s.blocks * s.tiles) {
-      off = 0;
-      do s = sequence(p, ++b, G::kRows, p.status);
-      while (s.blocks == 0);
-    }
+    at = to;
+    skip += nt;
+    if (skip != (uint32_t)s.tiles) return;  // the range ends within the item
   }
 }
 
-template <int DP, int WM, bool F8>
+template <int DP, int NT, int TW, bool F8>
 cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  using G = Geometry<DP, WM, F8>;
-  auto kernel = attention_kernel<DP, WM, F8>;
+  using G = Geometry<DP, NT, TW, F8>;
+  auto kernel = attention_kernel<DP, NT, TW, F8>;
   static bool attr_set[64] = {};
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
@@ -563,17 +725,20 @@ cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) 
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <int DP, int WM>
+template <int DP, int NT, int TW>
 cudaError_t launch_format(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  return p.cache.eight_bit ? launch<DP, WM, true>(p, sm_count, stream) : launch<DP, WM, false>(p, sm_count, stream);
+  return p.cache.eight_bit ? launch<DP, NT, TW, true>(p, sm_count, stream) : launch<DP, NT, TW, false>(p, sm_count, stream);
 }
 template <int DP>
 cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  // rows of a usual sequence; one with more takes several blocks of rows
+  // rows of a usual sequence; one with more takes several blocks of rows.  A warp holds 8 NT rows of sums (DP * NT / 4 registers
+  // a thread); more rows than that share keys and values between the warps of a team.
   const long long rows = (p.tokens + p.cache.sequences - 1) / p.cache.sequences * (long long)p.group;
-  if (rows <= 16) return launch_format<DP, 1>(p, sm_count, stream);
-  if (rows <= 32) return launch_format<DP, 2>(p, sm_count, stream);
-  return launch_format<DP, 4>(p, sm_count, stream);
+  constexpr int kMost = DP == 256 ? 2 : 4;
+  if (rows <= 8) return launch_format<DP, 1, 1>(p, sm_count, stream);
+  if (rows <= 16) return launch_format<DP, 2, 1>(p, sm_count, stream);
+  if (rows <= 32) return launch_format<DP, kMost, 4 / kMost>(p, sm_count, stream);
+  return launch_format<DP, kMost, 8 / kMost>(p, sm_count, stream);
 }
 
 }  // namespace
