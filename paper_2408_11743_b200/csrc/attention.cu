@@ -30,6 +30,9 @@ constexpr float kNone = -INFINITY;
 // weights are then at most 2^8, far from the end of fp16, and their rounding is relative.
 constexpr float kSlack = 8.f;
 
+constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+constexpr int blocks_per_sm(int dp, int nt, bool f8) { return dp == 256 ? 1 : nt == 1 && f8 ? 4 : 2; }
+
 // DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 rows per warp.  TW: warps that share keys and values and have
 // rows of their own (a team); the kWarps / TW teams share out the keys of a tile.  F8: e4m3 cache.
 template <int DP_, int NT, int TW, bool F8>
@@ -42,20 +45,18 @@ struct Geometry {
   static constexpr int kVectors = kRowBytes / 16;    // 16-byte vectors of a key
   static constexpr int kHalf = kTile * kRowBytes;    // the keys (or the values) of a tile
   static constexpr int kStage = 2 * kHalf;
-  static constexpr int kBlocks = DP == 256 ? 1 : 2;  // CTAs per SM
+  static constexpr int kBlocks = blocks_per_sm(DP, NT, F8);  // CTAs per SM
   static constexpr int kQVectors = DP / 8;
   static constexpr int kQBytes = kRows * DP * 2;
   static constexpr int kJoinStride = DP + 4;         // floats between rows of the teams' sums: rows 2 t fall on other banks
   static constexpr int kJoin = kTeams * kRows * (kJoinStride + 2) * 4;  // where the teams' sums meet, in the ring
-  static constexpr int kRoom = (kBlocks == 1 ? 224 : 112) * 1024 - kQBytes;
+  static constexpr int kRoom = 224 / kBlocks * 1024 - kQBytes;
   static constexpr int kStages = kRoom / kStage > 8 ? 8 : kRoom / kStage;
   static constexpr int kSmem = kQBytes + kStages * kStage;
   static constexpr bool kQInRegisters = NT * DP <= 256;
   static_assert(kStages >= 2 && kStages * kStage >= kJoin, "ring");
 };
 
-constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
-constexpr int blocks_per_sm(int dp) { return dp == 256 ? 1 : 2; }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   const int bytes = there ? 16 : 0;  // the rest is filled with zeros
@@ -91,6 +92,12 @@ template <int VECTORS>
 __device__ __forceinline__ uint32_t place(int row, int vec) {
   const int v = VECTORS >= 8 ? vec ^ (row & 7) : vec ^ ((row >> 1) & 3);
   return (uint32_t)(row * VECTORS + v) * 16;
+}
+// the same `vec` vectors further on, `vec` even, from an address in a line-aligned stage: one instruction and an offset
+template <int VECTORS>
+__device__ __forceinline__ uint32_t further(uint32_t address, int vec) {
+  constexpr int kLine = VECTORS >= 8 ? 8 : 4;
+  return (address ^ (uint32_t)(vec % kLine * 16)) + vec / kLine * (kLine * 16);
 }
 
 // A row that does not see a key has weight 0 there, and 0 times an infinity or a NaN is NaN.  Keys that no row of a block sees are
@@ -155,7 +162,7 @@ struct Stripes {
 };
 
 template <int DP, int NT, int TW, bool F8>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(const AttentionParams p) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(DP, NT, F8)) attention_kernel(const AttentionParams p) {
   using G = Geometry<DP, NT, TW, F8>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t scan[kWarps];
@@ -266,32 +273,40 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
     constexpr int kElement = F8 ? 1 : 2;
     const int my_row = lane / G::kVectors, my_vec = lane % G::kVectors;
     const bool my_part = my_vec * (16 / kElement) < c.head_dim;
-    const long long step_bytes = c.s_token * kElement;
-    const long long my_bytes = my_row * step_bytes + my_vec * 16;
     const int* const table = c.table + b * c.table_stride;
-    auto page_of = [&](int step) {  // the page of key lane % 16 of the warp's sixteen, -1 where it is not asked for
+    const long long head_bytes = h * c.s_head * kElement + my_row * c.s_token * kElement + my_vec * 16;
+    auto page_of = [&](int step) {  // the page of key lane % 16 of the warp's sixteen, INT_MIN where it is not asked for
       const int key = (tile + step) * kTile + warp * 16 + (lane & 15);
       return step < nt && key >= low_min && key < high_max ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
     };
-    auto bring = [&](int step, int page) {
+    auto bring = [&](int step, int page, uint32_t stage) {
       if (step < nt) {
         const int key0 = (tile + step) * kTile + warp * 16;
-        const uint32_t stage = ring + (step % G::kStages) * G::kStage;
-        const long long off = page == INT_MIN ? -1 : cache_offset(c, page, h, key0 + (lane & 15), p.status);
-        const bool one_page = c.page_shift >= 4 && __all_sync(~0u, off >= 0);
-        if (one_page) {  // sixteen keys of one page: their places are s_token apart
-          const long long first = __shfl_sync(~0u, off, 0) * kElement + my_bytes;
-          const uint8_t* k = static_cast<const uint8_t*>(c.k) + first;
-          const uint8_t* v = static_cast<const uint8_t*>(c.v) + first;
+        if (c.page_shift >= 4 && __all_sync(~0u, (unsigned)page < (unsigned)c.pages)) {
+          // sixteen keys of one page: their places are s_token apart
+          const long long first = (page * c.s_page + (key0 & ((1 << c.page_shift) - 1)) * c.s_token) * kElement + head_bytes;
+          const uint8_t* k = static_cast<const uint8_t*>(c.k) + (my_part ? first : 0);
+          const uint8_t* v = static_cast<const uint8_t*>(c.v) + (my_part ? first : 0);
+          if (c.s_token == DP) {
 #pragma unroll
-          for (int r = 0; r < 16; r += kPer) {
-            const uint32_t dst = stage + place<G::kVectors>(warp * 16 + r + my_row, my_vec);
-            copy16(dst, my_part ? k : c.k, my_part);
-            copy16(dst + G::kHalf, my_part ? v : c.v, my_part);
-            k += kPer * step_bytes;
-            v += kPer * step_bytes;
+            for (int r = 0; r < 16; r += kPer) {
+              const uint32_t dst = stage + place<G::kVectors>(warp * 16 + r + my_row, my_vec);
+              copy16(dst, k + r * G::kRowBytes, my_part);
+              copy16(dst + G::kHalf, v + r * G::kRowBytes, my_part);
+            }
+          } else {
+            const long long pass = my_part ? kPer * c.s_token * kElement : 0;
+#pragma unroll
+            for (int r = 0; r < 16; r += kPer) {
+              const uint32_t dst = stage + place<G::kVectors>(warp * 16 + r + my_row, my_vec);
+              copy16(dst, k, my_part);
+              copy16(dst + G::kHalf, v, my_part);
+              k += pass;
+              v += pass;
+            }
           }
         } else {
+          const long long off = page == INT_MIN ? -1 : cache_offset(c, page, h, key0 + (lane & 15), p.status);
 #pragma unroll 1
           for (int r = 0; r < 16; r += kPer) {
             const long long from = __shfl_sync(~0u, off, r + my_row);
@@ -319,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
 #pragma unroll 1
     for (int i = 0; i < G::kStages - 1; ++i) {
       const int next = page_of(i + 1);
-      bring(i, page);
+      bring(i, page, ring + i * G::kStage);
       page = next;
     }
 
@@ -328,7 +343,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) high[j][i] = base_high + (row0 + min(rows - 1, wm * 8 * NT + j * 8 + t4 * 2 + i)) / p.group;
+      for (int i = 0; i < 2; ++i)
+        high[j][i] = s.n == 1 ? base_high : base_high + (row0 + min(rows - 1, wm * 8 * NT + j * 8 + t4 * 2 + i)) / p.group;
     const float factor = p.scale_log2 * (F8 && c.k_scale ? __ldg(c.k_scale + h) : 1.f);
 
     // operands of Q: rows on the 8-wide side; of 16 elements a thread has 2 t, 2 t + 1, 2 t + 8, 2 t + 9, or, to match the
@@ -369,6 +385,12 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
       for (int v = 0; v < DP / 16; ++v) o[v][j][0] = o[v][j][1] = o[v][j][2] = o[v][j][3] = 0.f;
     }
     bool open = true;  // some row has not seen a key yet
+    // stages of this step and of the one that is brought: offsets in the ring
+    uint32_t keys = ring, free_stage = ring + (G::kStages - 1) * G::kStage;
+    const int key0 = team * G::kKeys;
+    // where this lane reads keys and values: 16 keys, vectors 0 and 1
+    const uint32_t k_lane = place<G::kVectors>(key0 + (lane & 15), lane >> 4);
+    const uint32_t v_lane = F8 ? k_lane : place<G::kVectors>(key0 + (lane & 7) + (lane >> 4) * 8, (lane >> 3) & 1);
 
 #pragma unroll 1
     for (int step = 0; step < nt; ++step) {
@@ -381,15 +403,15 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
         named_bar_sync(1 + team, 32 * TW);
       {
         const int next = page_of(step + G::kStages);
-        bring(step + G::kStages - 1, page);
+        bring(step + G::kStages - 1, page, free_stage);
         page = next;
       }
+      free_stage = keys;
       if (G::kQInRegisters && step == 0) {
 #pragma unroll
         for (int ks = 0; ks < DP / 16; ++ks) load_q(ks, q[G::kQInRegisters ? ks : 0]);
       }
-      const uint32_t keys = ring + (step % G::kStages) * G::kStage, values = keys + G::kHalf;
-      const int key0 = team * G::kKeys;
+      const uint32_t values = keys + G::kHalf;
 
       // S^T = K Q^T: a thread has keys g, g + 8 of 16 and rows 2 t, 2 t + 1 of 8.  (One tile alone would be a chain of dependent
       // products: it is summed in two.)
@@ -411,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
 #pragma unroll
         for (int kk = 0; kk < TW; ++kk) {
           uint32_t r[4];
-          ldmatrix_x4(keys + place<G::kVectors>(key0 + kk * 16 + (lane & 15), (F8 ? ks : 2 * ks) + (lane >> 4)), r);
+          ldmatrix_x4(further<G::kVectors>(keys + k_lane, F8 ? ks : 2 * ks) + kk * 16 * G::kRowBytes, r);
 #pragma unroll
           for (int i = 0; i < (F8 ? 2 : 1); ++i) {
             uint32_t a[4];
@@ -531,12 +553,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
 #pragma unroll
         for (int kk = 0; kk < TW; ++kk) {
           uint32_t r[4];
-          if (F8) {
-            // r[2 i], r[2 i + 1] of vector v + i: bytes (key 2 t: elements 2 g, 2 g + 1), (key 2 t + 1: the same); keys + 8
-            ldmatrix_x4_trans(values + place<G::kVectors>(key0 + kk * 16 + (lane & 15), v + (lane >> 4)), r);
-          } else {
-            ldmatrix_x4_trans(values + place<G::kVectors>(key0 + kk * 16 + (lane & 7) + (lane >> 4) * 8, 2 * v + ((lane >> 3) & 1)), r);
-          }
+          // 8-bit: r[2 i], r[2 i + 1] of vector v + i: bytes (key 2 t: elements 2 g, 2 g + 1), (key 2 t + 1: the same); keys + 8
+          ldmatrix_x4_trans(further<G::kVectors>(values + v_lane, F8 ? v : 2 * v) + kk * 16 * G::kRowBytes, r);
 #pragma unroll
           for (int i = 0; i < (F8 ? 2 : 1); ++i) {
             uint32_t a[4];
@@ -554,6 +572,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
           }
         }
       }
+      keys = keys == ring + (G::kStages - 1) * G::kStage ? ring : keys + G::kStage;
     }
 
     // ---- the teams' sums meet: [team][row] in the ring, with m and l behind
@@ -593,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
       c1 = stripes.owner(i1 - 1);
       while (stripes.begin(c1) > i0 && stripes.moved(stripes.begin(c1), i0, i1) == i1) --c1;
     }
-    constexpr int kSlot = G::kRows * (DP + 2);
+    constexpr int kSlot = G::kRows * (DP + 4);  // rows of DP sums, the base, the sum of the weights, and two that are not used
     auto slot = [&](uint32_t cta) { return p.partials + (size_t)(2 * cta + (cta == c0)) * kSlot; };
     auto write_out = [&](int r, int d, float4 x, float li) {
       const int token = (row0 + r) / p.group, head = h * p.group + (row0 + r) - token * p.group;
@@ -650,11 +669,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
         write_out(r, d, x, li);
       } else {
         float* to = slot(blockIdx.x);
-        *reinterpret_cast<float4*>(to + r * DP + d) = x;
-        if (d == 0) {
-          to[G::kRows * DP + 2 * r] = mi;
-          to[G::kRows * DP + 2 * r + 1] = li;
-        }
+        *reinterpret_cast<float4*>(to + r * (DP + 4) + d) = x;
+        if (d == 0) *reinterpret_cast<float2*>(to + r * (DP + 4) + DP) = make_float2(mi, li);
       }
     }
     if (!whole) {
@@ -665,24 +681,53 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP)) attention_kernel(
       if (arrived == (int)(c1 - c0)) {  // the last one: every part is there
         __threadfence();
         if (tid == 0) p.counters[c0] = 0;
+        // All parts of as many rows as the ring holds come at once (a load and its use at a time would take a round trip to the
+        // L2 for each of up to some hundred parts): [part][row][DP + 2 used, 4 rounded]
+        const int parts = (int)(c1 - c0) + 1;
+        constexpr int kLine = DP + 4;
+        constexpr int kFit = G::kStages * G::kStage / (kLine * 4);
+        const int part_step = min(parts, kFit), row_step = max(1, kFit / parts);
 #pragma unroll 1
-        for (int i = tid; i < rows * (DP / 4); i += kThreads) {
-          const int r = i / (DP / 4), d = (i % (DP / 4)) * 4;
-          if (d >= c.head_dim) continue;
-          float mi = kNone;
-          for (uint32_t w = c0; w <= c1; ++w) mi = fmaxf(mi, __ldcg(slot(w) + G::kRows * DP + 2 * r));
-          const float base = mi == kNone ? 0.f : mi;
-          float li = 0.f;
+        for (int r0 = 0; r0 < rows; r0 += row_step) {
+          const int nr = min(row_step, rows - r0);
+          float mi = kNone, li = 0.f;  // (kept from one batch to the next only where a row does not fit: one vector a thread then)
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (uint32_t w = c0; w <= c1; ++w) {
-            const float* from = slot(w);
-            const float2 part = __ldcg(reinterpret_cast<const float2*>(from + G::kRows * DP + 2 * r));
-            const float f = exp2_fast(part.x - base);
-            const float4 y = ld_cg_f4(reinterpret_cast<const float4*>(from + r * DP + d));
-            li += part.y * f;
-            x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+#pragma unroll 1
+          for (int w0 = 0; w0 < parts; w0 += part_step) {
+            const int nw = min(part_step, parts - w0);
+#pragma unroll 1
+            for (int i = tid; i < nw * nr * (kLine / 4); i += kThreads) {
+              const int vec = i % (kLine / 4), wr = i / (kLine / 4), w = wr / nr, r = wr - w * nr;
+              copy16(ring + wr * (kLine * 4) + vec * 16, slot(c0 + w0 + w) + (r0 + r) * kLine + vec * 4, true);
+            }
+            copies_commit();
+            copies_wait<0>();
+            __syncthreads();
+#pragma unroll 1
+            for (int i = tid; i < nr * (DP / 4); i += kThreads) {
+              const int r = i / (DP / 4), d = (i % (DP / 4)) * 4;
+              if (w0 == 0) {
+                mi = kNone;
+                li = 0.f;
+                x = make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+              float top = mi;
+              for (int w = 0; w < nw; ++w) top = fmaxf(top, join[(w * nr + r) * kLine + DP]);
+              const float base = top == kNone ? 0.f : top, old = exp2_fast(mi - base);
+              mi = top;
+              li *= old;
+              x.x *= old; x.y *= old; x.z *= old; x.w *= old;
+              for (int w = 0; w < nw; ++w) {
+                const float* from = join + (w * nr + r) * kLine;
+                const float f = exp2_fast(from[DP] - base);
+                const float4 y = *reinterpret_cast<const float4*>(from + d);
+                li += from[DP + 1] * f;
+                x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+              }
+              if (w0 + nw == parts && d < c.head_dim) write_out(r0 + r, d, x, li);
+            }
+            __syncthreads();
           }
-          write_out(r, d, x, li);
         }
       }
     }
@@ -743,10 +788,12 @@ cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t str
 
 }  // namespace
 
-// Two slots per CTA that a grid can have, of up to 64 rows with their maxima and sums.
+// Two slots per CTA that a grid can have, of its rows with their maxima and sums: most with 64 rows.
 size_t attention_slot_bytes(int head_dim) {
   const int dp = padded_dim(head_dim);
-  return (size_t)2 * kMaxWorkers * blocks_per_sm(dp) * 64 * (dp + 2) * sizeof(float);
+  static_assert(blocks_per_sm(64, 1, true) * 8 <= blocks_per_sm(64, 4, true) * 64 &&
+                blocks_per_sm(128, 1, true) * 8 <= blocks_per_sm(128, 4, true) * 64, "slots");
+  return (size_t)2 * kMaxWorkers * blocks_per_sm(dp, 4, false) * 64 * (dp + 4) * sizeof(float);
 }
 
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream) {
