@@ -31,7 +31,7 @@ constexpr float kNone = -INFINITY;
 constexpr float kSlack = 8.f;
 
 constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
-constexpr int blocks_per_sm(int dp, int nt, bool f8) { return dp == 256 ? 1 : nt == 1 && f8 ? 4 : 2; }
+constexpr int blocks_per_sm(int dp, int nt, bool f8) { return dp == 256 ? 1 : nt == 1 ? (f8 ? 4 : 3) : 2; }
 
 // DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 rows per warp.  TW: warps that share keys and values and have
 // rows of their own (a team); the kWarps / TW teams share out the keys of a tile.  F8: e4m3 cache.
@@ -696,9 +696,13 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(DP, NT, F8)) attention
           for (int w0 = 0; w0 < parts; w0 += part_step) {
             const int nw = min(part_step, parts - w0);
 #pragma unroll 1
-            for (int i = tid; i < nw * nr * (kLine / 4); i += kThreads) {
-              const int vec = i % (kLine / 4), wr = i / (kLine / 4), w = wr / nr, r = wr - w * nr;
-              copy16(ring + wr * (kLine * 4) + vec * 16, slot(c0 + w0 + w) + (r0 + r) * kLine + vec * 4, true);
+            for (int wr = warp, w = w0, r = warp; wr < nw * nr; wr += kWarps, r += kWarps) {  // a row of a part per warp
+              while (r >= nr) {
+                r -= nr;
+                ++w;
+              }
+              const float* from = slot(c0 + w) + (r0 + r) * kLine;
+              for (int vec = lane; vec < kLine / 4; vec += 32) copy16(ring + wr * (kLine * 4) + vec * 16, from + vec * 4, true);
             }
             copies_commit();
             copies_wait<0>();
