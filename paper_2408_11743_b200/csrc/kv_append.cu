@@ -73,6 +73,8 @@ __device__ __forceinline__ void store_cache(void* base, long long off, const flo
 template <bool F8>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams p) {
   __shared__ float2 turn[128];  // cosine and sine of each pair
+  __shared__ int sequence, position;
+  __shared__ long long place;
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const int t = blockIdx.x, tid = threadIdx.x;
@@ -96,28 +98,33 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
     if (r.pair) hi[i] = __ldg(reinterpret_cast<const uint4*>(src + r.at + p.rotary_dim / 2));
   }
 
-  // whose token this is: the first sequence whose rows end behind it
-  int b = t, end = t + 1;
-  if (p.starts) {
-    b = 0;
-    for (int i = 0; i < c.sequences; i += kThreads)
-      b += __syncthreads_count(i + tid < c.sequences && __ldg(p.starts + i + tid + 1) <= t);
-    if (b == c.sequences || t < __ldg(p.starts)) return;  // (the same for the whole CTA)
-    end = __ldg(p.starts + b + 1);
-    if (end <= t) return;  // (descending starts: nobody's)
+  // whose token this is, and where it goes: every thread looks at a sequence, and the one whose rows hold the token follows the
+  // table, so that the loads of a step are on their way together
+  const float frequency = p.inv_freq && tid < p.rotary_dim / 2 ? __ldg(p.inv_freq + tid) : 0.f;
+  if (tid == 0) sequence = -1;
+  __syncthreads();
+  for (int b = p.starts ? tid : t; b < (p.starts ? c.sequences : t + 1); b += kThreads) {
+    if (!p.starts && tid > 0) break;
+    const int from = p.starts ? __ldg(p.starts + b) : t, end = p.starts ? __ldg(p.starts + b + 1) : t + 1;
+    const int len = cache_length(c, b, p.status);
+    if (from > t || t >= end) continue;
+    const int pos = len - (end - t);
+    position = pos;
+    place = pos >= 0 ? cache_offset(c, __ldg(c.table + b * c.table_stride + (pos >> c.page_shift)), 0, pos, p.status) : -1;
+    sequence = b;
   }
-  const int pos = cache_length(c, b, p.status) - (end - t);
+  __syncthreads();
+  if (sequence < 0) return;  // nobody's
+  const int pos = position;
+  const long long to = place;
   if (p.inv_freq && tid < p.rotary_dim / 2) {
     constexpr double kTurnsPerRadian = 0.15915494309189533577;
-    const double turns = (double)pos * (double)__ldg(p.inv_freq + tid) * kTurnsPerRadian;
+    const double turns = (double)pos * (double)frequency * kTurnsPerRadian;
     float s, co;
     sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
     turn[tid] = make_float2(co, s);
   }
   __syncthreads();
-  int page = -1;
-  if (pos >= 0) page = __ldg(c.table + b * c.table_stride + (pos >> c.page_shift));
-  const long long place = pos >= 0 ? cache_offset(c, page, 0, pos, p.status) : -1;
 
 #pragma unroll
   for (int i = 0; i < kMostUnits; ++i) {
@@ -149,12 +156,12 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
       const uint4 none = make_uint4(0, 0, 0, 0);
       *reinterpret_cast<uint4*>(dst) = pos >= 0 ? to_halves(x) : none;
       if (r.pair) *reinterpret_cast<uint4*>(dst + p.rotary_dim / 2) = pos >= 0 ? to_halves(y) : none;
-    } else if (place >= 0) {
+    } else if (to >= 0) {
       const bool key = r.head < p.q_heads + c.kv_heads;
       const int h = r.head - p.q_heads - (key ? 0 : c.kv_heads);
       const float* scales = key ? c.k_scale : c.v_scale;
       const float scale = F8 && scales ? __ldg(scales + h) : 1.f;
-      const long long off = place + h * c.s_head + r.at;
+      const long long off = to + h * c.s_head + r.at;
       store_cache<F8>(key ? c.k : c.v, off, x, scale);
       if (r.pair) store_cache<F8>(key ? c.k : c.v, off + p.rotary_dim / 2, y, scale);
     }
@@ -172,7 +179,7 @@ cudaError_t launch_kv_append(AppendParams p, int tokens, int interleaved, int sm
   // a few tokens: their heads are spread over more CTAs, until the SMs have one each
   p.units_per_thread = kMostUnits;
   while (p.units_per_thread > 1 &&
-         (long long)tokens * ((p.units + kThreads * p.units_per_thread - 1) / (kThreads * p.units_per_thread)) < sm_count)
+         (long long)tokens * ((p.units + kThreads * p.units_per_thread - 1) / (kThreads * p.units_per_thread)) < 2 * sm_count)
     p.units_per_thread /= 2;
   const int per = kThreads * p.units_per_thread;
   cudaLaunchConfig_t cfg = {};
