@@ -13,26 +13,10 @@
 // over the ends of segments, so the next sequence's keys are on their way while this one's sums are joined.
 // The products are mma.sync.m16n8k16 with the keys (of S^T = K Q^T) and the values (of O^T = V^T P^T) on the 16-wide side and
 // the rows on the 8-wide one: a decode step has few rows, and eight of them fill an operand.
-#include <limits.h>
-
-#include "kv_cache.cuh"
+#include "attention.cuh"
 
 namespace marlin_b200 {
 namespace {
-
-constexpr int kLeastTiles = 2;  // tiles that a CTA takes at least, where there are fewer tiles than CTAs would like
-constexpr uint32_t kMostUnits = 1u << 30;
-constexpr int kMostCtas = kMaxWorkers;
-constexpr int kItemCounters = 2 * kMostCtas;  // counters of items behind those of groups
-static_assert(3 * kMostCtas * sizeof(int) <= kWsPartialOff - kWsCounterOff, "counters");
-constexpr int kGroup = 4;  // parts that are joined at once; more of them are joined in groups first, each by its last CTA
-constexpr float kNone = -INFINITY;
-// A row's sums are kept relative to 2^base, base its largest logit (in units of log2) when the base was last moved.  It moves only
-// when a logit exceeds it by more than this, so that most tiles neither look for a maximum across lanes nor rescale:
-// weights are then at most 2^8, far from the end of fp16, and their rounding is relative.
-constexpr float kSlack = 8.f;
-
-constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
 // DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 rows per warp.  TW: warps side by side over the rows.
 // F8: e4m3 cache.  A stage of kTile keys is multiplied by kParts * TW warps (a group); the groups take the stages in turn.
@@ -73,15 +57,6 @@ struct Geometry {
   static_assert(kConsumers % (kParts * TW) == 0 && kStages >= 2 && kStages >= kGroups && DP % (16 * kRounds) == 0, "ring");
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-  const int bytes = there ? 16 : 0;  // the rest is filled with zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-// an arrival at `bar` when all copies that this thread has issued so far are complete
-__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t saddr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -93,16 +68,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // byte of a 16-byte vector of a row in half a stage: vectors are permuted within 128-byte lines, so that eight rows of one
 // vector lie in eight different groups of banks
 template <int VECTORS>
@@ -115,91 +80,6 @@ template <int VECTORS>
 __device__ __forceinline__ uint32_t further(uint32_t address, int vec) {
   constexpr int kLine = VECTORS >= 8 ? 8 : 4;
   return (address ^ (uint32_t)(vec % kLine * 16)) + vec / kLine * (kLine * 16);
-}
-
-// A row that does not see a key has weight 0 there, and 0 times an infinity or a NaN is NaN.  Keys that no row of a block sees are
-// never loaded; values of keys that some of its rows see (those around the new tokens, and as many at the edge of a window)
-// are looked through in shared memory, what is not finite is replaced by 0, and added to the rows that see it at the end.
-template <bool F8>
-__device__ __forceinline__ bool clean_vector(uint32_t saddr) {
-  const uint4 v = lds128(saddr);
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  bool found = false;
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t part = F8 ? 0xffu : 0xffffu, most = F8 ? 0x7fu : 0x7c00u;
-    for (int j = 0; j < 32; j += F8 ? 8 : 16) {
-      if (((w[i] >> j) & most) == most) {
-        w[i] &= ~(part << j);
-        found = true;
-      }
-    }
-  }
-  if (found)
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-  return found;
-}
-
-// What a sequence asks for: new tokens [first, first + n) of the call, tiles [tile0, tile0 + tiles) of its len keys, blocks of
-// rows per key head.  A sequence with new tokens has a tile at least: it writes the zeros.
-struct Sequence {
-  int len, n, first, tile0, tiles, blocks;
-};
-__device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, int rows, int tile) {
-  Sequence s;
-  s.len = cache_length(p.cache, b, p.status);
-  s.first = b;
-  s.n = 1;
-  if (p.starts) {
-    const int from = min(max(__ldg(p.starts + b), 0), p.tokens), to = min(max(__ldg(p.starts + b + 1), from), p.tokens);
-    s.first = from;
-    s.n = to - from;
-  }
-  s.tile0 = (p.window ? max(0, s.len - s.n - p.window + 1) : 0) / tile;
-  s.tiles = max(1, (s.len + tile - 1) / tile - s.tile0);
-  s.blocks = (s.n * p.group + rows - 1) / rows;
-  return s;
-}
-
-// The ranges of the CTAs.  What is numbered are the items (the tiles of one block of rows), each as `lead` units and one unit per tile: an
-// item has a cost of its own beside its tiles (its Q, the sums of its warps that meet), and a CTA with many short ones would end
-// late.  Worker w of W begins at unit w * (U / W) + min(w, U % W).  A range that would begin within the lead, or within `snap` tiles of
-// the beginning or the end of an item, begins there instead: a part of an item costs a round trip through the workspace, which
-// is worth a tile or two where a CTA has few.
-struct Stripes {
-  uint32_t total, workers, size, more, snap, lead;
-  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * size + min(w, more); }
-  __device__ __forceinline__ uint32_t owner(uint32_t x) const {  // whose range, before any move, holds unit x
-    const uint32_t wide = more * (size + 1);
-    return x < wide ? x / (size + 1) : more + (x - wide) / size;
-  }
-  // boundary x of the ranges where it lies inside of item [i0, i1)
-  __device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t i0, uint32_t i1) const {
-    if (x <= i0 || x >= i1) return x;
-    if (x - i0 <= lead || (x - i0 <= lead + snap && x - i0 - lead <= i1 - x)) return i0;
-    return i1 - x <= snap ? i1 : x;
-  }
-};
-
-// One segment of a CTA's range: tiles [tile, tile + nt) of (sequence b, key head h, rows row0 .. row0 + rows - 1); row r is query
-// head h * group + r % group of new token r / group.  Row r sees the positions [high - window, high) (all below high without a
-// window), high = base_high + its token.  CTAs c0 .. c1 have tiles of the item.  nt = 0: there are no more segments.
-struct Segment {
-  int b, h, tile, nt, row0, rows, base_high, n, first, c0, c1;
-};
-// positions that some row of a segment sees: [low_min, high_max), that all of them see: [low_max, high_min)
-struct Visible {
-  int low_min, low_max, high_min, high_max;
-};
-__device__ __forceinline__ Visible visible(const AttentionParams& p, const Segment& x) {
-  Visible v;
-  v.high_min = v.high_max = x.base_high;
-  if (x.n > 1) {
-    v.high_min += x.row0 / p.group;
-    v.high_max += (x.row0 + x.rows - 1) / p.group;
-  }
-  v.low_min = p.window ? max(0, v.high_min - p.window) : 0;
-  v.low_max = p.window ? max(0, v.high_max - p.window) : 0;
-  return v;
 }
 
 // Barriers and notes in shared memory.  Every wait is bounded (mbar_wait): when one runs out, `abort` is set, all warps leave at their
@@ -230,55 +110,8 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
   const KvCacheView& c = p.cache;
   const int lane = threadIdx.x & 31;
 
-  // this CTA's range of tiles: lane i counts the tiles of sequences [i * per, (i + 1) * per)
-  const int per = (c.sequences + 31) / 32;
-  uint32_t mine = 0;
-  for (int b = lane * per; b < min(c.sequences, (lane + 1) * per); ++b) {
-    const Sequence s = sequence(p, b, G::kRows, kTile);
-    const unsigned long long units = (unsigned long long)c.kv_heads * s.blocks * (s.tiles + G::kLead) + mine;
-    mine = (uint32_t)min(units, (unsigned long long)kMostUnits);
-  }
-  uint32_t before = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const uint32_t x = __shfl_up_sync(~0u, before, d);
-    if (lane >= d) before = min(before + x, kMostUnits);
-  }
-  Stripes stripes;
-  stripes.total = __shfl_sync(~0u, before, 31);
-  before -= mine;
-  bool more = stripes.total > 0;
-  if (stripes.total == kMostUnits) {  // more tiles than are numbered (2^30: weeks of work): refused
-    report_cache(p.status);
-    more = false;
-  }
-  stripes.workers = min(gridDim.x, max(1u, stripes.total / kLeastTiles));
-  more = more && blockIdx.x < stripes.workers;
-  stripes.size = stripes.total / stripes.workers;
-  stripes.more = stripes.total % stripes.workers;
-  stripes.snap = stripes.size < 8 ? 2 : 0;
-  stripes.lead = G::kLead;
-  uint32_t at = stripes.begin(blockIdx.x), skip = 0;  // units; those of the item in front of `at`
-  const uint32_t end = stripes.begin(blockIdx.x + 1);
-  Sequence s;
-  int b = 0, item = 0;
-  if (more) {  // where the range begins: (sequence, item of it, tile of that)
-    const int owner = __ffs(__ballot_sync(~0u, mine > 0 && before <= at && at < before + mine)) - 1;
-    b = owner * per;
-    uint32_t off = at - __shfl_sync(~0u, before, owner);
-    for (;; ++b) {
-      s = sequence(p, b, G::kRows, kTile);
-      const uint32_t units = (uint32_t)c.kv_heads * s.blocks * (s.tiles + G::kLead);
-      if (off < units) break;
-      off -= units;
-    }
-    const uint32_t units = s.tiles + G::kLead;
-    item = (int)(off / units);
-    skip = off - item * units;
-    const uint32_t to = stripes.moved(at, at - skip, at - skip + units);
-    skip += to - at;
-    at = to;
-  }
+  Range<G::kRows, kTile, G::kLead> range;
+  range.begin(p);
 
   constexpr int kPer = G::kVectors < 32 ? 32 / G::kVectors : 1;  // keys per pass of the warp
   constexpr int kElement = F8 ? 1 : 2;
@@ -293,46 +126,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
   int slot = 0;
 #pragma unroll 1
   for (;; ++segment) {
-    // ---- the next segment
-    if (more && skip == (uint32_t)s.tiles + G::kLead) {
-      more = at < end;
-      if (more) {
-        skip = 0;
-        if (++item == c.kv_heads * s.blocks) {
-          item = 0;
-          do s = sequence(p, ++b, G::kRows, kTile);
-          while (s.blocks == 0);
-        }
-      }
-    }
-    Segment x;
-    x.nt = 0;
-    if (more) {
-      const uint32_t i0 = at - skip, i1 = i0 + G::kLead + s.tiles, to = min(stripes.moved(end, i0, i1), i1);
-      if (at < to) {
-        x.b = b;
-        x.h = item / s.blocks;
-        const int from = skip ? (int)skip - G::kLead : 0;
-        x.tile = s.tile0 + from;
-        x.nt = (int)(to - i0) - G::kLead - from;
-        x.row0 = (item - x.h * s.blocks) * G::kRows;
-        x.rows = min(G::kRows, s.n * p.group - x.row0);
-        x.base_high = s.len - s.n + 1;
-        x.n = s.n;
-        x.first = s.first;
-        uint32_t c0 = blockIdx.x, c1 = blockIdx.x;
-        if (x.nt != s.tiles) {
-          c0 = stripes.owner(i0);
-          while (c0 + 1 < stripes.workers && stripes.begin(c0 + 1) < i1 && stripes.moved(stripes.begin(c0 + 1), i0, i1) == i0) ++c0;
-          c1 = stripes.owner(i1 - 1);
-          while (stripes.begin(c1) > i0 && stripes.moved(stripes.begin(c1), i0, i1) == i1) --c1;
-        }
-        x.c0 = (int)c0;
-        x.c1 = (int)c1;
-      }
-      skip += to - at;
-      at = to;
-    }
+    const Segment x = range.next(p);
     if (!arrived_at(sh, &sh.closed[slot], slot_phase, p.status)) break;
     if (lane == 0 && producer == 0) sh.segments[slot] = x;
     if (x.nt > 0) {  // Q; rows and elements that are not there are zeros
@@ -665,22 +459,9 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
         l[j][i] += __shfl_xor_sync(~0u, l[j][i], 8);
         l[j][i] += __shfl_xor_sync(~0u, l[j][i], 16);
       }
-    const uint32_t c0 = x.c0, c1 = x.c1;
-    const bool whole = c0 == c1;
-    constexpr int kLine = DP + 4;  // a row of a part: DP sums, the base, the sum of the weights, and two that are not used
-    constexpr int kSlot = G::kRows * kLine;
-    // a CTA has parts of at most two items that it shares: one that it begins (c0), one that it goes on with
-    auto slot_of = [&](uint32_t cta) { return p.partials + (size_t)(2 * cta + (cta == c0)) * kSlot; };
-    auto write_out = [&](int r, int d, float4 z, float li) {
-      const int token = (x.row0 + r) / p.group, head = x.h * p.group + (x.row0 + r) - token * p.group;
-      const bool nothing = x.base_high + token <= 0;
-      const float f = nothing ? 0.f : (F8 && c.v_scale ? __ldg(c.v_scale + x.h) : 1.f) / li;
-      if (nothing) z = make_float4(0.f, 0.f, 0.f, 0.f);
-      uint2 two;
-      two.x = half2_bits(z.x * f, z.y * f);
-      two.y = half2_bits(z.z * f, z.w * f);
-      *reinterpret_cast<uint2*>(p.out + ((long long)(x.first + token) * p.q_heads + head) * c.head_dim + d) = two;
-    };
+    const bool whole = x.c0 == x.c1;
+    constexpr int kLine = part_line(DP);
+    auto write_out = [&](int r, int d, float4 z, float li) { write_four(p, x, r, d, z, li); };
     auto bank = [](int r, int d) { return G::kColumns >= 32 ? d ^ ((r >> 1 & 3) * 8) : d; };
 #pragma unroll
     for (int round = 0; round < G::kRounds; ++round) {
@@ -722,97 +503,22 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
           z.x += u.x * f; z.y += u.y * f; z.z += u.z * f; z.w += u.w * f;
         }
         if (odd_values) {
-          const int top = x.base_high + (x.row0 + r) / p.group, low = p.window ? max(0, top - p.window) : 0;
 #pragma unroll 1
-          for (int pos = max(low, tile * kTile); pos < min(top, (tile + nt) * kTile); ++pos) {
-            if (pos >= low_max && pos < high_min) {  // (every row sees these: they were left where they are)
-              pos = high_min - 1;
-              continue;
-            }
-            const long long off = cache_offset(c, __ldg(c.table + x.b * c.table_stride + (pos >> c.page_shift)), x.h, pos, p.status);
-            if (off < 0) continue;
-            float v[4];
-            for (int e = 0; e < 4; ++e) {
-              if (F8) {
-                const uint32_t two = e4m3x2_to_f16x2(static_cast<const uint8_t*>(c.v)[off + d + e]);
-                v[e] = __low2float(*reinterpret_cast<const __half2*>(&two));
-              } else {
-                v[e] = __half2float(static_cast<const __half*>(c.v)[off + d + e]);
-              }
-              if (isfinite(v[e])) v[e] = 0.f;
-            }
-            z.x += v[0]; z.y += v[1]; z.z += v[2]; z.w += v[3];
+          for (int e = 0; e < 4; ++e) {
+            const float v = not_finite_sum<F8>(p, x, sees, kTile, r, d + e);
+            z.x += e == 0 ? v : 0.f; z.y += e == 1 ? v : 0.f; z.z += e == 2 ? v : 0.f; z.w += e == 3 ? v : 0.f;
           }
         }
         if (whole) {
           write_out(r, d, z, li);
         } else {
-          float* to = slot_of(blockIdx.x);
+          float* to = part_of(p, x, blockIdx.x, G::kRows, DP);
           *reinterpret_cast<float4*>(to + r * kLine + d) = z;
           if (d == 0) *reinterpret_cast<float2*>(to + r * kLine + DP) = make_float2(mi, li);
         }
       }
     }
-    // ---- parts of an item: the last CTA of a group of them joins the group, the last group the item, in the order of the keys
-    if (!whole) {
-      uint32_t first = c0 + (blockIdx.x - c0) / kGroup * kGroup, stride = 1;
-      int count = (int)min((uint32_t)kGroup, c1 + 1 - first);
-      const int groups = (int)(c1 - c0) / kGroup + 1;
-      int* counter = p.counters + 2 * first + (first == c0);  // (a CTA may be the first of a group of each item that it shares)
-#pragma unroll 1
-      for (;;) {
-        if (!meet()) return;  // (all parts of the CTA are written; the release below carries them)
-        if (tid == 0) sh.arrived = atom_add_acq_rel_gpu(counter, 1);
-        if (!meet()) return;
-        if (sh.arrived != count - 1) break;
-        if (tid == 0) *counter = 0;
-        const bool last = groups == 1 || stride > 1;
-#pragma unroll 1
-        for (int i = tid; i < rows * (DP / 4); i += kMine) {
-          const int r = i / (DP / 4), d = (i % (DP / 4)) * 4;
-          if (d >= c.head_dim) continue;
-          float mi = kNone, li = 0.f;
-          float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-          for (int w0 = 0; w0 < count; w0 += kGroup) {
-            float2 sums[kGroup];
-            float4 u[kGroup];
-            float top = mi;
-#pragma unroll
-            for (int t = 0; t < kGroup; ++t) {
-              const float* from = slot_of(first + min(w0 + t, count - 1) * stride) + r * kLine;
-              sums[t] = __ldcg(reinterpret_cast<const float2*>(from + DP));
-              u[t] = ld_cg_f4(reinterpret_cast<const float4*>(from + d));
-              top = fmaxf(top, sums[t].x);
-            }
-            const float base = top == kNone ? 0.f : top, old = exp2_fast(mi - base);
-            mi = top;
-            li *= old;
-            z.x *= old; z.y *= old; z.z *= old; z.w *= old;
-#pragma unroll
-            for (int t = 0; t < kGroup; ++t) {
-              if (w0 + t >= count) break;
-              const float f = exp2_fast(sums[t].x - base);
-              li += sums[t].y * f;
-              z.x += u[t].x * f; z.y += u[t].y * f; z.z += u[t].z * f; z.w += u[t].w * f;
-            }
-          }
-          if (last) {
-            write_out(r, d, z, li);
-          } else {  // the sums of a group take the place of its first part; its base and weight when everybody has read them
-            *reinterpret_cast<float4*>(slot_of(first) + r * kLine + d) = z;
-            if (d == 0) sh.ml[r] = make_float2(mi, li);
-          }
-        }
-        if (last) break;
-        if (!meet()) return;
-        for (int r = tid; r < rows; r += kMine) *reinterpret_cast<float2*>(slot_of(first) + r * kLine + DP) = sh.ml[r];
-        counter = p.counters + kItemCounters + c0;
-        first = c0;
-        stride = kGroup;
-        count = groups;
-      }
-    }
+    if (!whole && !join_parts<G::kRows, DP, kMine, 1>(p, x, tid, &sh.arrived, sh.ml, meet, write_out)) return;
     __syncwarp();
     if (lane == 0) mbar_arrive(&sh.closed[slot]);
     if (++slot == G::kOpen) {
@@ -857,68 +563,42 @@ __global__ void __launch_bounds__(Geometry<DP, NT, TW, F8>::kThreads, 1) attenti
 template <int DP, int NT, int TW, bool F8>
 cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) {
   using G = Geometry<DP, NT, TW, F8>;
-  auto kernel = attention_kernel<DP, NT, TW, F8>;
-  static bool attr_set[64] = {};
-  int dev = 0;
-  cudaError_t err = cudaGetDevice(&dev);
-  if (err != cudaSuccess) return err;
-  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem);
-    if (err != cudaSuccess) return err;
-    // the warps share out the registers of the launch: with fewer of them the increase would wait for ever
-    cudaFuncAttributes fa;
-    err = cudaFuncGetAttributes(&fa, kernel);
-    if (err != cudaSuccess) return err;
-    if (G::kConsumerRegs > G::kLaunchRegs && fa.numRegs != G::kLaunchRegs) return cudaErrorInvalidConfiguration;
-    if (dev >= 0 && dev < 64) attr_set[dev] = true;
-  }
-  // no more CTAs than there can be tiles: blocks of rows of all sequences, each with the most tiles that the table holds
-  const long long most = sm_count < kMaxWorkers ? sm_count : kMaxWorkers;
-  const long long blocks = ((long long)p.tokens * p.group + G::kRows - 1) / G::kRows + p.cache.sequences;
-  const long long per_block = (((long long)p.cache.max_pages << p.cache.page_shift) + G::kTile - 1) / G::kTile + 1;
-  const long long tiles = (blocks < most ? blocks : most) * (per_block < most ? per_block : most) * p.cache.kv_heads;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles < most ? tiles : most));
-  cfg.blockDim = dim3(G::kThreads);
-  cfg.dynamicSmemBytes = G::kSmem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p);
+  // the warps share out the registers of the launch: with fewer of them the increase would wait for ever
+  return launch_ranges<attention_kernel<DP, NT, TW, F8>, G::kSmem, G::kThreads, G::kRows, G::kTile>(
+      p, sm_count, stream, G::kConsumerRegs > G::kLaunchRegs ? G::kLaunchRegs : 0);
 }
-
-template <int DP, int NT, int TW>
-cudaError_t launch_format(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  return p.cache.eight_bit ? launch<DP, NT, TW, true>(p, sm_count, stream) : launch<DP, NT, TW, false>(p, sm_count, stream);
+template <int DP, bool F8>
+cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
+  // A warp holds 8 NT rows of sums (DP * NT / 4 registers a thread); more rows than that share keys and values between
+  // the warps of a team.
+  const long long rows = usual_rows(p);
+  if (rows <= 8) return launch<DP, 1, 1, F8>(p, sm_count, stream);
+  if constexpr (F8 || DP == 256) {
+    if (rows <= 16) return launch<DP, 2, 1, F8>(p, sm_count, stream);
+    if (DP == 128 || rows <= 32) return launch<DP, DP == 64 ? 4 : 2, DP == 64 ? 1 : 2, F8>(p, sm_count, stream);
+    return launch<DP, DP == 64 ? 4 : 2, DP == 64 ? 2 : DP == 128 ? 2 : 4, F8>(p, sm_count, stream);
+  } else {
+    return launch_attention_tc(p, sm_count, stream);
+  }
 }
 template <int DP>
-cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  // rows of a usual sequence; one with more takes several blocks of rows.  A warp holds 8 NT rows of sums (DP * NT / 4 registers
-  // a thread); more rows than that share keys and values between the warps of a team.
-  const long long rows = (p.tokens + p.cache.sequences - 1) / p.cache.sequences * (long long)p.group;
-  constexpr int kMost = DP == 256 ? 2 : 4;
-  if (rows <= 8) return launch_format<DP, 1, 1>(p, sm_count, stream);
-  if (rows <= 16) return launch_format<DP, 2, 1>(p, sm_count, stream);
-  if (rows <= 32) return launch_format<DP, kMost, 4 / kMost>(p, sm_count, stream);
-  return launch_format<DP, kMost, 8 / kMost>(p, sm_count, stream);
+cudaError_t launch_format(const AttentionParams& p, int sm_count, cudaStream_t stream) {
+  return p.cache.eight_bit ? launch_rows<DP, true>(p, sm_count, stream) : launch_rows<DP, false>(p, sm_count, stream);
 }
 
 }  // namespace
 
-// Two slots per CTA that a grid can have, of its rows with their maxima and sums: most with 64 rows.
+// Two parts per CTA that a grid can have, of its rows.
 size_t attention_slot_bytes(int head_dim) {
-  const int dp = padded_dim(head_dim);
-  return (size_t)2 * kMostCtas * 64 * (dp + 4) * sizeof(float);
+  const int dp = padded_dim(head_dim), rows = dp == 256 ? 64 : 128;
+  return (size_t)2 * kMostCtas * rows * part_line(dp) * sizeof(float);
 }
 
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream) {
   switch (padded_dim(p.cache.head_dim)) {
-    case 64: return launch_rows<64>(p, sm_count, stream);
-    case 128: return launch_rows<128>(p, sm_count, stream);
-    default: return launch_rows<256>(p, sm_count, stream);
+    case 64: return launch_format<64>(p, sm_count, stream);
+    case 128: return launch_format<128>(p, sm_count, stream);
+    default: return launch_format<256>(p, sm_count, stream);
   }
 }
 

@@ -159,6 +159,8 @@ struct AttentionParams {
 };
 size_t attention_slot_bytes(int head_dim);
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream);
+// where a key head of an fp16 cache has more than eight rows (attention_tc.cu); head_dim up to 128
+cudaError_t launch_attention_tc(const AttentionParams& p, int sm_count, cudaStream_t stream);
 
 // ---- the stripe partition (host and device use the same two formulas) ------------------------
 // worker w of P owns units [w*U/P, (w+1)*U/P); the owner of unit x is floor(((x+1)*P - 1) / U).
