@@ -8,8 +8,10 @@
 // of a matrix of ones with P, and the largest logits are looked for only when one exceeds the base of its row by kSlack
 // (attention.cuh), which needs the sums in tensor memory to be rescaled.
 //
-// Warps: 0 - 3 softmax and results (lane quarter w of tensor memory), 4 - 7 copies (32 keys of every tile each), 8 issues the
-// products.  Keys and values take slots of the ring in turn.  Tensor memory: S twice, O, the sums of the weights; N columns each.
+// Warps: 0 - 7 softmax and results (lane quarter w % 4 of tensor memory; 0 - 3 the first half of the rows, 4 - 7 the second, each
+// half with bases of its own), 8 - 11 copies (32 keys of every tile each), 12 - 14 issue one of the three products each: an issue
+// costs its thread some 75 cycles and a commit 125, and with one thread for all of them (24 products and four commits a tile of
+// 128 x 128) everybody waited for it.  Keys and values take slots of the ring in turn.  Tensor memory: S twice, O, the sums of the weights; N columns each.
 #include "attention.cuh"
 #include "tc_utils.cuh"
 
@@ -19,9 +21,11 @@ namespace {
 constexpr int kTile = 128;
 constexpr int kLead = 1;                 // what an item costs beside its tiles, in tiles
 constexpr int kBlock = kTile * 128;      // 64 elements of the keys of a tile: rows of 128 bytes, as the swizzle has them
-constexpr int kSoftmaxThreads = 128;
+constexpr int kSoftmaxWarps = 8;
+constexpr int kSoftmaxThreads = kSoftmaxWarps * 32;
 constexpr int kProducers = 4;
-constexpr int kThreads = kSoftmaxThreads + kProducers * 32 + 32;
+constexpr int kIssuers = 3;
+constexpr int kThreads = kSoftmaxThreads + (kProducers + kIssuers) * 32;
 
 // DP: head_dim rounded up to 64 or 128; N: rows of a block
 template <int DP_, int N_>
@@ -39,7 +43,8 @@ struct TcGeometry {
   static constexpr int kSlots = (222 * 1024 - kRest) / kSlot > 12 ? 12 : (222 * 1024 - kRest) / kSlot;
   static constexpr int kSmem = kSlots * kSlot + kRest + 1024;  // (the ring begins at a multiple of 1024)
   static constexpr int kColumns = 4 * N < 32 ? 32 : 4 * N;     // of tensor memory: S, S, O, sums of weights
-  static constexpr int kChunk = N < 32 ? N : 32;               // columns that a thread holds at a time
+  static constexpr int kMine = N / 2;                          // rows of a half of the softmax warps
+  static constexpr int kChunk = kMine < 16 ? kMine : 16;       // columns that a thread holds at a time
   static_assert(kSlots >= 3 && kColumns <= 512, "ring");
 };
 
@@ -49,7 +54,6 @@ struct TcShared {
   uint64_t opened[G::kOpen], closed[G::kOpen];
   uint64_t s_full[2], s_free[2];                       // logits are there; have been read
   uint64_t p_full[G::kPBuffers], p_done[G::kPBuffers]; // weights are there; have been multiplied
-  uint64_t meet;
   Segment segments[G::kOpen];
   float2 ml[G::N];
   alignas(16) float base[G::N];  // of the rows, read four at a time; 0 where a row has seen nothing
@@ -57,7 +61,6 @@ struct TcShared {
   float alpha[G::N];      // what the sums are multiplied with when the base moves
   float tops[4][G::N];
   int high[G::N];         // positions below which the rows see
-  int over[3];
   int abort;
   int arrived;
   int not_finite[2];
@@ -96,9 +99,30 @@ __device__ __forceinline__ float warp_max(float x) {
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
+// bar.sync of some warps that also tells all of them whether `mine` is set for any of their threads
+__device__ __forceinline__ bool any_of(int id, int threads, bool mine) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 p, %1, 0;\n"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"((uint32_t)mine), "r"(id), "r"(threads)
+      : "memory");
+  return r != 0;
+}
 template <int C>
 __device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[C]) {
-  if constexpr (C == 32) tc_ld_x32(taddr, x); else tc_ld_x16(taddr, x);
+  if constexpr (C == 16)
+    tc_ld_x16(taddr, x);
+  else
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                 : "r"(taddr)
+                 : "memory");
 }
 __device__ __forceinline__ void load_column(uint32_t taddr, float& x) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=f"(x) : "r"(taddr) : "memory");
@@ -223,8 +247,9 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
   copies_wait_all();
 }
 
-// ---- the thread that issues the products -----------------------------------------------------------
-template <class G>
+// ---- the threads that issue the products -----------------------------------------------------------
+enum Product { kLogits, kResults, kSums };
+template <class G, int WHICH>
 __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& sh, uint32_t ring, uint32_t q_slots, uint32_t weights,
                                          uint32_t ones, uint32_t tmem) {
   constexpr int N = G::N;
@@ -234,133 +259,148 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
     mbar_wait(bar, parity, &sh.abort, p.status);
     return *(volatile int*)&sh.abort == 0;
   };
-  // slots go round: keys of tile u, values of tile u; `behind`: the values that have not been multiplied yet
-  int k_slot = 0, v_slot = 1;
-  uint32_t k_phase = 0, v_phase = 0;
-  auto two_on = [](int& slot, uint32_t& phase) {
-    slot += 2;
-    if (slot >= G::kSlots) {
-      slot -= G::kSlots;
-      phase ^= 1;
-    }
-  };
-  uint32_t u = 0;        // tiles whose logits have been issued
-  uint32_t done = 0;     // tiles whose results have been issued
-  bool behind_first = false;
-  auto results = [&]() -> bool {  // of tile `done`, the oldest that waits
-    const uint32_t pb = done % G::kPBuffers;
-    if (!wait(&sh.p_full[pb], done / G::kPBuffers & 1) || !wait(&sh.full[v_slot], v_phase)) return false;
-    fence_to_tensor_cores();
-    tc_fence_after_sync();
-    const uint32_t values = ring + v_slot * G::kSlot, w = weights + pb * G::kPBytes;
-#pragma unroll
-    for (int ks = 0; ks < kTile / 16; ++ks) {
-      const uint64_t b = desc_rows(w + ks / 4 * G::kQBlock + ks % 4 * 32, 1024);
-      const uint32_t more = behind_first && ks == 0 ? 0 : 1;
-      mma_ss(tmem + 2 * N, desc_columns(values + ks * 2048, G::kHalves == 2 ? kBlock : 0), b, kColumnsDesc, more);
-      mma_ss(tmem + 3 * N, desc_rows(ones, 0), b, kRowsDesc, more);
-    }
-    tc_commit(&sh.empty[v_slot]);
-    tc_commit(&sh.p_done[pb]);
-    two_on(v_slot, v_phase);
-    ++done;
-    return true;
-  };
-  int open = 0;
-  uint32_t open_phase = 0;
+  int slot = WHICH == kLogits ? 0 : 1, open = 0;  // slots go round: keys of tile u, values of tile u
+  uint32_t phase = 0, open_phase = 0, u = 0;
 #pragma unroll 1
   for (;;) {
     if (!wait(&sh.opened[open], open_phase)) return;
-    const int nt = sh.segments[open].nt;
-    if (nt == 0) break;
+    const int nt = *(volatile int*)&sh.segments[open].nt;
+    if (nt == 0) return;
+    if (WHICH != kLogits) mbar_arrive(&sh.closed[open]);  // (nothing else of the segment is needed here)
 #pragma unroll 1
     for (int i = 0; i < nt; ++i, ++u) {
-      const uint32_t buf = u & 1;
-      if (!wait(&sh.full[k_slot], k_phase) || !wait(&sh.s_free[buf], (u >> 1 & 1) ^ 1)) return;
+      const uint32_t buf = u & 1, pb = u % G::kPBuffers;
+      if (WHICH == kLogits) {
+        if (!wait(&sh.full[slot], phase) || !wait(&sh.s_free[buf], (u >> 1 & 1) ^ 1)) return;
+      } else {
+        if (WHICH == kResults && !wait(&sh.full[slot], phase)) return;
+        if (!wait(&sh.p_full[pb], u / G::kPBuffers & 1)) return;
+      }
       fence_to_tensor_cores();
       tc_fence_after_sync();
-      const uint32_t keys = ring + k_slot * G::kSlot, q = q_slots + open * G::kQBytes;
+      if (WHICH == kLogits) {
+        const uint32_t keys = ring + slot * G::kSlot, q = q_slots + open * G::kQBytes;
 #pragma unroll
-      for (int ks = 0; ks < G::DP / 16; ++ks)
-        mma_ss(tmem + buf * N, desc_rows(keys + ks / 4 * kBlock + ks % 4 * 32, 1024),
-               desc_rows(q + ks / 4 * G::kQBlock + ks % 4 * 32, 1024), kRowsDesc, ks ? 1 : 0);
-      tc_commit(&sh.empty[k_slot]);
-      tc_commit(&sh.s_full[buf]);
-      if (i + 1 == nt) tc_commit(&sh.closed[open]);
-      two_on(k_slot, k_phase);
-      if (u != done) {  // (the logits of this tile run while the softmax of the one before gives its weights)
-        if (!results()) return;
+        for (int ks = 0; ks < G::DP / 16; ++ks)
+          mma_ss(tmem + buf * N, desc_rows(keys + ks / 4 * kBlock + ks % 4 * 32, 1024),
+                 desc_rows(q + ks / 4 * G::kQBlock + ks % 4 * 32, 1024), kRowsDesc, ks ? 1 : 0);
+        tc_commit(&sh.s_full[buf]);
+        tc_commit(&sh.empty[slot]);
+        if (i + 1 == nt) tc_commit(&sh.closed[open]);
+      } else {
+        const uint32_t w = weights + pb * G::kPBytes, values = ring + slot * G::kSlot;
+#pragma unroll
+        for (int ks = 0; ks < kTile / 16; ++ks) {
+          const uint64_t b = desc_rows(w + ks / 4 * G::kQBlock + ks % 4 * 32, 1024);
+          if (WHICH == kResults)
+            mma_ss(tmem + 2 * N, desc_columns(values + ks * 2048, G::kHalves == 2 ? kBlock : 0), b, kColumnsDesc, i || ks ? 1 : 0);
+          else
+            mma_ss(tmem + 3 * N, desc_rows(ones, 0), b, kRowsDesc, i || ks ? 1 : 0);
+        }
+        tc_commit(&sh.p_done[pb]);
+        if (WHICH == kResults) tc_commit(&sh.empty[slot]);
       }
-      behind_first = i == 0;
+      slot += 2;
+      if (slot >= G::kSlots) {
+        slot -= G::kSlots;
+        phase ^= 1;
+      }
     }
-    if (G::kOpen == 1 && !results()) return;  // (the next segment opens when this one's results are written)
     if (++open == G::kOpen) {
       open = 0;
       open_phase ^= 1;
     }
   }
-  if (u != done) results();
 }
 
 // ---- softmax and results ---------------------------------------------------------------------------
+// Whether a wait has run out is agreed upon where a segment begins, so that these warps always meet at the same barriers; what
+// they compute of a segment whose copies did not come is thrown away with the call.
 template <class G>
 __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh, uint32_t ring, uint32_t weights, uint32_t tmem) {
-  constexpr int N = G::N, DP = G::DP, kChunk = G::kChunk;
+  constexpr int N = G::N, DP = G::DP, kMine = G::kMine, kChunk = G::kChunk;
   const KvCacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t lanes = tmem + ((uint32_t)warp << 21);  // (lane 32 * warp of tensor memory)
-
-  uint32_t meet_phase = 0;
+  const int key = tid & 127, half = tid >> 7, mine = half * kMine;  // this thread's key, and the first of its rows
+  const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);       // (lane 32 * (warp % 4) of tensor memory)
+  auto wait = [&](uint64_t* bar, uint32_t parity) { mbar_wait(bar, parity, &sh.abort, p.status); };
+  auto meet_half = [&] { named_bar_sync(1 + half, 128); };
   auto meet = [&] {
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.meet);
-    meet_phase ^= 1;
-    return arrived_at(sh, &sh.meet, meet_phase ^ 1, p.status);
+    named_bar_sync(3, kSoftmaxThreads);
+    return true;
   };
 
   uint32_t u = 0;  // tiles so far
   int open = 0, odd = 0;
   uint32_t open_phase = 0;
   // where this thread's key lies in the weights: byte of row r = w_key + r * 128, with the 16-byte vectors of a row permuted by r
-  const uint32_t w_key = tid / 64 * G::kQBlock + tid % 8 * 2, w_vec = tid % 64 / 8;
+  const uint32_t w_key = key / 64 * G::kQBlock + key % 8 * 2 + mine * 128, w_vec = key % 64 / 8;
 #pragma unroll 1
   for (;; odd ^= 1) {
-    if (!arrived_at(sh, &sh.opened[open], open_phase, p.status)) return;
+    wait(&sh.opened[open], open_phase);
+    if (any_of(3, kSoftmaxThreads, *(volatile int*)&sh.abort)) return;
     const Segment& x = sh.segments[open];
     const int nt = x.nt, rows = x.rows;
     if (nt == 0) return;
     const Visible sees = visible(p, x);
     const bool several = x.n > 1;
-    for (int r = tid; r < N; r += kSoftmaxThreads) {
+    for (int r = mine + key; r < mine + kMine; r += 128) {
       sh.largest[r] = kNone;
       sh.base[r] = 0.f;
       sh.high[r] = several ? x.base_high + (x.row0 + min(r, rows - 1)) / p.group : x.base_high;
     }
-    if (!meet()) return;
+    meet_half();
     bool fresh = true;  // some row has not seen a key yet
 
 #pragma unroll 1
     for (int i = 0; i < nt; ++i, ++u) {
       const uint32_t buf = u & 1, pb = u % G::kPBuffers;
-      const int pos0 = (x.tile + i) * kTile, pos = pos0 + tid;
+      const int pos0 = (x.tile + i) * kTile, pos = pos0 + key;
       const bool all = pos0 >= sees.low_max && pos0 + kTile <= sees.high_min;
-      if (!arrived_at(sh, &sh.s_full[buf], u >> 1 & 1, p.status)) return;
-      if (!arrived_at(sh, &sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1, p.status)) return;  // (the weights before are multiplied)
+      const uint32_t logits = lanes + buf * N + mine, w_to = weights + pb * G::kPBytes + w_key;
+      wait(&sh.s_full[buf], u >> 1 & 1);
       tc_fence_after_sync();
-      const uint32_t w_to = weights + pb * G::kPBytes + w_key;
+      auto seen = [&](int r) {
+        const int high = sh.high[mine + r];
+        return all || (pos < high && !(p.window && pos < high - p.window));
+      };
+      if (i == 0) {  // bases to begin with: the largest logit of a row over the 32 keys of one warp, a quarter of the rows each
+#pragma unroll 1
+        for (int c0 = 0; c0 < kMine; c0 += kChunk) {
+          float y[kChunk];
+          load_columns(logits + c0, y);
+          tc_wait_ld();
+#pragma unroll
+          for (int r = 0; r < kChunk; r += 4) {
+            // (row r + warp % 4, without an index that is not known to the compiler)
+            const float z = (warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]);
+            const int row = c0 + r + (warp & 3);
+            const float top = warp_max(seen(row) ? z * p.scale_log2 : kNone);
+            if (lane == 0) {
+              sh.largest[mine + row] = top;
+              sh.base[mine + row] = top == kNone ? 0.f : top;
+            }
+          }
+        }
+        meet_half();
+        bool none = false;
+        for (int r = lane; r < kMine; r += 32) none |= *(volatile float*)&sh.largest[mine + r] == kNone;
+        fresh = __any_sync(~0u, none);
+      }
+      wait(&sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1);  // (the weights that were there are multiplied)
 
       // weights relative to the bases as they are; `over`: some logit is too far above its base (or there is none yet), and
       // all of it is done again
       bool over = fresh;
       auto weigh = [&](bool look) {
 #pragma unroll 1
-        for (int c0 = 0; c0 < N; c0 += kChunk) {
+        for (int c0 = 0; c0 < kMine; c0 += kChunk) {
           float y[kChunk];
-          load_columns(lanes + buf * N + c0, y);
+          load_columns(logits + c0, y);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < kChunk; r += 4) {
-            const float4 base = *reinterpret_cast<const float4*>(&sh.base[c0 + r]);
+            const float4 base = *reinterpret_cast<const float4*>(&sh.base[mine + c0 + r]);
             y[r] = fmaf(y[r], p.scale_log2, -base.x);
             y[r + 1] = fmaf(y[r + 1], p.scale_log2, -base.y);
             y[r + 2] = fmaf(y[r + 2], p.scale_log2, -base.z);
@@ -368,10 +408,8 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
           }
           if (!all) {
 #pragma unroll
-            for (int r = 0; r < kChunk; ++r) {
-              const int high = sh.high[c0 + r];
-              if (pos >= high || (p.window && pos < high - p.window)) y[r] = kNone;
-            }
+            for (int r = 0; r < kChunk; ++r)
+              if (!seen(c0 + r)) y[r] = kNone;
           }
           if (look) {
 #pragma unroll
@@ -381,28 +419,22 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
           for (int r = 0; r < kChunk; ++r) store_half(w_to + (c0 + r) * 128 + (w_vec ^ (r & 7)) * 16, exp2_fast(y[r]));
         }
       };
-      if (!fresh) weigh(true);
-      if (!fresh) {
-        if (over) sh.over[u % 3] = 1;
-        if (!meet()) return;
-        over = *(volatile int*)&sh.over[u % 3];
-      }
+      weigh(true);
+      over = any_of(1 + half, 128, over);
       if (over) {  // move the bases: the largest logit of every row over the 128 keys
 #pragma unroll 1
-        for (int c0 = 0; c0 < N; c0 += kChunk) {
+        for (int c0 = 0; c0 < kMine; c0 += kChunk) {
           float y[kChunk];
-          load_columns(lanes + buf * N + c0, y);
+          load_columns(logits + c0, y);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < kChunk; ++r) {
-            const int high = sh.high[c0 + r];
-            const bool seen = all || (pos < high && !(p.window && pos < high - p.window));
-            const float top = warp_max(seen ? y[r] * p.scale_log2 : kNone);
-            if (lane == 0) sh.tops[warp][c0 + r] = top;
+            const float top = warp_max(seen(c0 + r) ? y[r] * p.scale_log2 : kNone);
+            if (lane == 0) sh.tops[warp & 3][mine + c0 + r] = top;
           }
         }
-        if (!meet()) return;
-        for (int r = tid; r < N; r += kSoftmaxThreads) {
+        meet_half();
+        for (int r = mine + key; r < mine + kMine; r += 128) {
           const float old = sh.largest[r];
           const float now = fmaxf(fmaxf(fmaxf(old, sh.tops[0][r]), fmaxf(sh.tops[1][r], sh.tops[2][r])), sh.tops[3][r]);
           const float base = now == kNone ? 0.f : now;
@@ -410,38 +442,37 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
           sh.largest[r] = now;
           sh.base[r] = base;
         }
-        if (!meet()) return;
+        meet_half();
         bool none = false;
-        for (int r = lane; r < N; r += 32) none |= *(volatile float*)&sh.largest[r] == kNone;
+        for (int r = lane; r < kMine; r += 32) none |= *(volatile float*)&sh.largest[mine + r] == kNone;
         fresh = __any_sync(~0u, none);
         if (i > 0) {  // the sums so far, when the products that add to them are done
           const uint32_t before = u - 1;
-          if (!arrived_at(sh, &sh.p_done[before % G::kPBuffers], before / G::kPBuffers & 1, p.status)) return;
+          wait(&sh.p_done[before % G::kPBuffers], before / G::kPBuffers & 1);
           tc_fence_after_sync();
 #pragma unroll 1
-          for (int c0 = 0; c0 < 2 * N; c0 += kChunk) {
+          for (int c0 = 0; c0 < 2 * kMine; c0 += kChunk) {
+            const uint32_t sums = lanes + (c0 < kMine ? 2 * N : 3 * N - kMine) + mine + c0;
             float y[kChunk];
-            load_columns(lanes + 2 * N + c0, y);
+            load_columns(sums, y);
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < kChunk; ++r) y[r] *= sh.alpha[c0 % N + r];
-            store_columns(lanes + 2 * N + c0, y);
+            for (int r = 0; r < kChunk; ++r) y[r] *= sh.alpha[mine + c0 % kMine + r];
+            store_columns(sums, y);
           }
           tc_wait_st();
         }
         weigh(false);
       }
-      // (everybody has met since the tile before was looked at, and will meet again before the tile after the next one is)
-      if (tid == 0) sh.over[(u + 2) % 3] = 0;
       tc_fence_before_sync();
-      if (several && !all) {  // values of keys that not every row sees: what is not finite is left out
+      if (several && !all && half == 0) {  // values of keys that not every row sees: what is not finite is left out
         const uint32_t v_slot = (2 * u + 1) % G::kSlots;
-        if (!arrived_at(sh, &sh.full[v_slot], (2 * u + 1) / G::kSlots & 1, p.status)) return;
+        wait(&sh.full[v_slot], (2 * u + 1) / G::kSlots & 1);
         if ((pos >= sees.high_min && pos < sees.high_max) || (pos >= sees.low_min && pos < sees.low_max)) {
           bool found = false;
 #pragma unroll 1
           for (int vec = 0; vec < DP / 8; ++vec)
-            found |= clean_vector<false>(ring + v_slot * G::kSlot + vec / 8 * kBlock + tid * 128 + ((vec ^ tid) & 7) * 16);
+            found |= clean_vector<false>(ring + v_slot * G::kSlot + vec / 8 * kBlock + key * 128 + ((vec ^ key) & 7) * 16);
           if (found) sh.not_finite[odd] = 1;
         }
       }
@@ -454,61 +485,59 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     }
 
     // ---- results: lane d has element d of all rows
-    {
-      const uint32_t last = u - 1;
-      if (!arrived_at(sh, &sh.p_done[last % G::kPBuffers], last / G::kPBuffers & 1, p.status)) return;
-      tc_fence_after_sync();
-      if (several && !meet()) return;
-      if (tid == 0) sh.not_finite[odd ^ 1] = 0;
-      const bool whole = x.c0 == x.c1;
-      constexpr int kLine = part_line(DP), kFew = 16;  // columns at a time
-      auto give = [&](int r, int token, int head, float z, float l) {
-        if (whole) {
-          uint16_t* to = p.out + ((long long)(x.first + token) * p.q_heads + x.h * p.group + head) * c.head_dim;
-          const __half h = __float2half_rn(x.base_high + token <= 0 ? 0.f : z * (1.f / l));
-          if (tid < c.head_dim) to[tid] = *reinterpret_cast<const uint16_t*>(&h);
-        } else {
-          float* to = part_of(p, x, blockIdx.x, N, DP) + r * kLine;
-          if (tid < DP) to[tid] = z;
-          if (tid == 0) *reinterpret_cast<float2*>(to + DP) = make_float2(sh.largest[r], l);
-        }
-      };
-      int token = x.row0 / p.group, head = x.row0 - token * p.group;
-      if (several && *(volatile int*)&sh.not_finite[odd]) {  // (one column at a time, with what was left out)
+    const uint32_t last = u - 1;
+    wait(&sh.p_done[last % G::kPBuffers], last / G::kPBuffers & 1);
+    tc_fence_after_sync();
+    if (several) meet();
+    if (tid == 0) sh.not_finite[odd ^ 1] = 0;
+    const bool whole = x.c0 == x.c1;
+    constexpr int kLine = part_line(DP);
+    auto give = [&](int r, int token, int head, float z, float l) {
+      if (whole) {
+        uint16_t* to = p.out + ((long long)(x.first + token) * p.q_heads + x.h * p.group + head) * c.head_dim;
+        const __half h = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z, l));
+        if (key < c.head_dim) to[key] = *reinterpret_cast<const uint16_t*>(&h);
+      } else {
+        float* to = part_of(p, x, blockIdx.x, N, DP) + r * kLine;
+        if (key < DP) to[key] = z;
+        if (key == 0) *reinterpret_cast<float2*>(to + DP) = make_float2(sh.largest[r], l);
+      }
+    };
+    int token = (x.row0 + mine) / p.group, head = x.row0 + mine - token * p.group;
+    if (several && *(volatile int*)&sh.not_finite[odd]) {  // (one column at a time, with what was left out)
 #pragma unroll 1
-        for (int r = 0; r < rows; ++r) {
-          float z, l;
-          load_column(lanes + 2 * N + r, z);
-          load_column(lanes + 3 * N + r, l);
-          tc_wait_ld();
-          give(r, token, head, z + not_finite_sum<false>(p, x, sees, kTile, r, tid), l);
+      for (int r = mine; r < min(rows, mine + kMine); ++r) {
+        float z, l;
+        load_column(lanes + 2 * N + r, z);
+        load_column(lanes + 3 * N + r, l);
+        tc_wait_ld();
+        give(r, token, head, z + not_finite_sum<false>(p, x, sees, kTile, r, key), l);
+        if (++head == p.group) {
+          head = 0;
+          ++token;
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int c0 = mine; c0 < min(rows, mine + kMine); c0 += kChunk) {
+        float y[kChunk], l[kChunk];
+        load_columns(lanes + 2 * N + c0, y);
+        load_columns(lanes + 3 * N + c0, l);
+        tc_wait_ld();
+#pragma unroll
+        for (int r = 0; r < kChunk; ++r) {
+          if (c0 + r < rows) give(c0 + r, token, head, y[r], l[r]);
           if (++head == p.group) {
             head = 0;
             ++token;
           }
         }
-      } else {
-#pragma unroll 1
-        for (int c0 = 0; c0 < rows; c0 += kFew) {
-          float y[kFew], l[kFew];
-          load_columns(lanes + 2 * N + c0, y);
-          load_columns(lanes + 3 * N + c0, l);
-          tc_wait_ld();
-#pragma unroll
-          for (int r = 0; r < kFew; ++r) {
-            if (c0 + r < rows) give(c0 + r, token, head, y[r], l[r]);
-            if (++head == p.group) {
-              head = 0;
-              ++token;
-            }
-          }
-        }
       }
-      tc_fence_before_sync();
-      auto write_out = [&](int r, int d, float4 z, float li) { write_four(p, x, r, d, z, li); };
-      if (!whole && !join_parts<N, DP, kSoftmaxThreads, 2>(p, x, tid, &sh.arrived, sh.ml, meet, write_out)) return;
     }
-    if (!meet()) return;  // (bases and notes are free again)
+    tc_fence_before_sync();
+    auto write_out = [&](int r, int d, float4 z, float li) { write_four(p, x, r, d, z, li); };
+    if (!whole) join_parts<N, DP, kSoftmaxThreads, 2>(p, x, tid, &sh.arrived, sh.ml, meet, write_out);
+    meet();  // (bases and notes are free again)
     if (lane == 0) mbar_arrive(&sh.closed[open]);
     if (++open == G::kOpen) {
       open = 0;
@@ -532,20 +561,18 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
     }
     for (int i = 0; i < G::kOpen; ++i) {
       mbar_init(&sh.opened[i], 32 * kProducers + 1);  // the copies of all lanes, and the note itself
-      mbar_init(&sh.closed[i], 4 + 1);                // the softmax warps, and the last product that reads Q
+      mbar_init(&sh.closed[i], kSoftmaxWarps + kIssuers);  // the softmax warps, the issuers, and for one of them its last product that reads Q
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.s_free[i], 4);
+      mbar_init(&sh.s_free[i], kSoftmaxWarps);
     }
     for (int i = 0; i < G::kPBuffers; ++i) {
-      mbar_init(&sh.p_full[i], 4);
-      mbar_init(&sh.p_done[i], 1);
+      mbar_init(&sh.p_full[i], kSoftmaxWarps);
+      mbar_init(&sh.p_done[i], 2);
     }
-    mbar_init(&sh.meet, 4);
     sh.abort = 0;
     sh.not_finite[0] = sh.not_finite[1] = 0;
-    sh.over[0] = sh.over[1] = sh.over[2] = 0;
   }
   if (threadIdx.x < G::kOnes / 16) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ones + threadIdx.x * 16), "r"(0x3c003c00u) : "memory");
@@ -561,12 +588,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   const uint32_t tmem = sh.tmem;
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  if (warp < 4) {
+  if (warp < kSoftmaxWarps) {
     soften<G>(p, sh, ring, weights, tmem);
-  } else if (warp < 4 + kProducers) {
-    produce<G>(p, sh, warp - 4, ring, q_slots);
+  } else if (warp < kSoftmaxWarps + kProducers) {
+    produce<G>(p, sh, warp - kSoftmaxWarps, ring, q_slots);
   } else if (threadIdx.x % 32 == 0) {
-    multiply<G>(p, sh, ring, q_slots, weights, ones, tmem);
+    if (warp == kSoftmaxWarps + kProducers)
+      multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
+    else if (warp == kSoftmaxWarps + kProducers + 1)
+      multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
+    else
+      multiply<G, kSums>(p, sh, ring, q_slots, weights, ones, tmem);
   }
   __syncwarp();
   tc_fence_before_sync();
