@@ -590,8 +590,8 @@ cudaError_t launch_format(const AttentionParams& p, int sm_count, cudaStream_t s
 
 // Two parts per CTA that a grid can have, of its rows.
 size_t attention_slot_bytes(int head_dim) {
-  const int dp = padded_dim(head_dim), rows = dp == 256 ? 64 : 128;
-  return (size_t)2 * kMostCtas * rows * part_line(dp) * sizeof(float);
+  const int dp = padded_dim(head_dim);
+  return (size_t)2 * kMostCtas * 64 * part_line(dp) * sizeof(float);
 }
 
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream) {

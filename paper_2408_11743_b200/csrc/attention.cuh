@@ -377,9 +377,11 @@ __device__ __forceinline__ bool join_parts(const AttentionParams& p, const Segme
 }
 
 // ---- host ----------------------------------------------------------------------------------------
-// rows of a key head that a usual sequence of the call has; one with more takes several blocks of rows
+// Rows of a key head that most sequences of the call have at most; one with more takes several blocks of rows, and reads its keys again for
+// each.  Where the tokens are not the same number for every sequence, some have more than the mean: up to twice as many are expected.
 inline long long usual_rows(const AttentionParams& p) {
-  return (p.tokens + p.cache.sequences - 1) / p.cache.sequences * (long long)p.group;
+  const long long mean = (p.tokens + p.cache.sequences - 1) / p.cache.sequences;
+  return (p.tokens % p.cache.sequences ? 2 * mean - 1 : mean) * p.group;
 }
 
 // One CTA per SM, but no more than there can be tiles: blocks of rows of all sequences, each with the most tiles that the table

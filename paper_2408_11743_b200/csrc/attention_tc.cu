@@ -4,14 +4,18 @@
 // A tile has 128 keys.  S^T = K Q^T with the keys as the 128 rows of the product and the rows of Q as its columns, so that thread k of
 // the softmax warps has key k and all N rows of it in its lane of tensor memory; the weights go to shared memory as P, and
 // O^T += V^T P^T has the elements of the head as its 128 rows.  Both products are as narrow as there are rows: 128 x N x 16 a step.
-// What a thread sees of a row is one key, so nothing is summed over keys by threads at all: the sums of the weights are a third product,
-// of a matrix of ones with P, and the largest logits are looked for only when one exceeds the base of its row by kSlack
-// (attention.cuh), which needs the sums in tensor memory to be rescaled.
+// A thread sees one key of every row.  So the largest logits of rows, which would have to be looked for across threads, are looked for
+// only when a logit exceeds the base of its row by kSlack (attention.cuh); the sums in tensor memory are rescaled then.  The
+// weights of a row are summed by a block of ones beside the values where the head leaves room for it in the 128 rows of the second
+// product (64 elements), and otherwise by the threads, over the keys that each of them sees.
+//
+// What bounds it: the products read every key and value from shared memory once, 128 bytes a cycle: 512 cycles for a tile of
+// 64 KB, which takes 2800 to come from memory.  (A third product, of ones with the weights, cost as much as either of the two.)
 //
 // Warps: 0 - 7 softmax and results (lane quarter w % 4 of tensor memory; 0 - 3 the first half of the rows, 4 - 7 the second, each
-// half with bases of its own), 8 - 11 copies (32 keys of every tile each), 12 - 14 issue one of the three products each: an issue
-// costs its thread some 75 cycles and a commit 125, and with one thread for all of them (24 products and four commits a tile of
-// 128 x 128) everybody waited for it.  Keys and values take slots of the ring in turn.  Tensor memory: S twice, O, the sums of the weights; N columns each.
+// half with bases of its own), 8 - 11 copies (32 keys of every tile each), 12 and 13 issue a product each: an issue costs its thread
+// some 75 cycles and a commit 125, and with one thread for all of them everybody waited for it.
+// Keys and values take slots of the ring in turn.  Tensor memory: S twice, and O; N columns each.
 #include "attention.cuh"
 #include "tc_utils.cuh"
 
@@ -24,10 +28,10 @@ constexpr int kBlock = kTile * 128;      // 64 elements of the keys of a tile: r
 constexpr int kSoftmaxWarps = 8;
 constexpr int kSoftmaxThreads = kSoftmaxWarps * 32;
 constexpr int kProducers = 4;
-constexpr int kIssuers = 3;
+constexpr int kIssuers = 2;
 constexpr int kThreads = kSoftmaxThreads + (kProducers + kIssuers) * 32;
 
-// DP: head_dim rounded up to 64 or 128; N: rows of a block
+// DP: head_dim rounded up to 64 or 128; N: rows of a block, 16, 32 or 64
 template <int DP_, int N_>
 struct TcGeometry {
   static constexpr int DP = DP_, N = N_;
@@ -35,16 +39,16 @@ struct TcGeometry {
   static constexpr int kSlot = kHalves * kBlock;   // the keys (or the values) of a tile
   static constexpr int kQBlock = N * 128;          // 64 elements of the rows
   static constexpr int kQBytes = kHalves * kQBlock;
-  static constexpr int kOpen = N == 128 ? 1 : 2;   // segments that can be open at a time
+  static constexpr int kOpen = 2;                  // segments that can be open at a time
   static constexpr int kPBytes = 2 * kQBlock;      // weights: 64 keys of the rows, twice
-  static constexpr int kPBuffers = N == 128 ? 1 : 2;
-  static constexpr int kOnes = 1024;               // eight rows of 64 ones
+  static constexpr int kPBuffers = 2;
+  static constexpr bool kSumRows = DP == 64;       // the weights are summed in the product
+  static constexpr int kOnes = kSumRows ? 2048 : 0;  // 16 rows of 64 ones, beside the values of 16 keys
   static constexpr int kRest = kOpen * kQBytes + kPBuffers * kPBytes + kOnes;
   static constexpr int kSlots = (222 * 1024 - kRest) / kSlot > 12 ? 12 : (222 * 1024 - kRest) / kSlot;
   static constexpr int kSmem = kSlots * kSlot + kRest + 1024;  // (the ring begins at a multiple of 1024)
-  static constexpr int kColumns = 4 * N < 32 ? 32 : 4 * N;     // of tensor memory: S, S, O, sums of weights
-  static constexpr int kMine = N / 2;                          // rows of a half of the softmax warps
-  static constexpr int kChunk = kMine < 16 ? kMine : 16;       // columns that a thread holds at a time
+  static constexpr int kColumns = 4 * N;           // of tensor memory: S, S, O, and N that a power of two brings along
+  static constexpr int kMine = N / 2;              // rows of a half of the softmax warps
   static_assert(kSlots >= 3 && kColumns <= 512, "ring");
 };
 
@@ -57,10 +61,10 @@ struct TcShared {
   Segment segments[G::kOpen];
   float2 ml[G::N];
   alignas(16) float base[G::N];  // of the rows, read four at a time; 0 where a row has seen nothing
-  float largest[G::N];    // the same, -inf where a row has seen nothing
-  float alpha[G::N];      // what the sums are multiplied with when the base moves
-  float tops[4][G::N];
-  int high[G::N];         // positions below which the rows see
+  float largest[G::N];           // the same, -inf where a row has seen nothing
+  float alpha[G::N];             // what the sums are multiplied with when the base moves
+  float tops[4][G::N];           // of the warps: largest logits; sums of weights
+  int high[G::N];                // positions below which the rows see
   int abort;
   int arrived;
   int not_finite[2];
@@ -116,7 +120,9 @@ __device__ __forceinline__ bool any_of(int id, int threads, bool mine) {
 }
 template <int C>
 __device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[C]) {
-  if constexpr (C == 16)
+  if constexpr (C == 32)
+    tc_ld_x32(taddr, x);
+  else if constexpr (C == 16)
     tc_ld_x16(taddr, x);
   else
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -158,6 +164,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
   const int my_row = lane / kVectors, my_vec = lane % kVectors;
   const bool my_part = my_vec * 8 < c.head_dim;
   const bool big_pages = c.page_shift >= 4;  // sixteen keys lie in one page
+  const long long values_off = static_cast<const uint8_t*>(c.v) - static_cast<const uint8_t*>(c.k);
   int slot = 0, open = 0;
   uint32_t slot_phase = 1, open_phase = 1;
 #pragma unroll 1
@@ -205,34 +212,43 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
         pages = pages_next;
         pages_next = page_of(i + batch);
       }
+      // the two sixteens of this warp: where they begin in the cache, or that some key of them is not there
+      const int key0 = key_first + i * kTile;
+      const uint8_t* from[2];
+      bool whole = big_pages && key0 >= low && key0 + 32 <= high;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int page = __shfl_sync(~0u, pages, big_pages ? in_batch * 2 + j : 0);
+        whole = whole && (unsigned)page < (unsigned)c.pages;
+        const long long first = (page * c.s_page + ((key0 + j * 16) & ((1 << c.page_shift) - 1)) * c.s_token) * 2 + head_bytes;
+        from[j] = static_cast<const uint8_t*>(c.k) + (whole && my_part ? first : 0);
+      }
 #pragma unroll 1
       for (int which = 0; which < 2; ++which) {  // keys, values
         if (!arrived_at(sh, &sh.empty[slot], slot_phase, p.status)) {
           go_on = false;
           break;
         }
-        const uint8_t* const cache = static_cast<const uint8_t*>(which ? c.v : c.k);
-#pragma unroll 1
-        for (int j = 0; j < 2; ++j) {
-          const int key0 = key_first + i * kTile + j * 16, row0 = producer * 32 + j * 16;
-          const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (row0 + my_row) * 128;
-          const int page = __shfl_sync(~0u, pages, big_pages ? in_batch * 2 + j : 0);
-          if (big_pages && key0 >= low && key0 + 16 <= high && (unsigned)page < (unsigned)c.pages) {
-            const uint8_t* src = cache + (my_part ? (page * c.s_page + (key0 & ((1 << c.page_shift) - 1)) * c.s_token) * 2 + head_bytes : 0);
+        const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (producer * 32 + my_row) * 128;
+        if (whole) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint8_t* src = from[j] + (which ? values_off : 0);
 #pragma unroll
             for (int r = 0; r < 16; r += kPer) {
-              copy16(to + r * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
+              copy16(to + (j * 16 + r) * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
               src += pass;
             }
-          } else {
+          }
+        } else {
+          const uint8_t* const cache = static_cast<const uint8_t*>(which ? c.v : c.k);
 #pragma unroll 1
-            for (int r = 0; r < 16; r += kPer) {
-              const int key = key0 + r + my_row;
-              const int mine = __shfl_sync(~0u, pages, big_pages ? in_batch * 2 + j : j * 16 + r + my_row);
-              const long long from = key >= low && key < high ? cache_offset(c, mine, x.h, key, p.status) : -1;
-              const bool there = from >= 0 && my_part;
-              copy16(to + r * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, cache + (there ? from * 2 + my_vec * 16 : 0), there);
-            }
+          for (int r = 0; r < 32; r += kPer) {
+            const int row = r + my_row, key = key0 + row;
+            const int mine = __shfl_sync(~0u, pages, big_pages ? in_batch * 2 + row / 16 : row);
+            const long long at = key >= low && key < high ? cache_offset(c, mine, x.h, key, p.status) : -1;
+            const bool there = at >= 0 && my_part;
+            copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
           }
         }
         copies_arrive(&sh.full[slot]);
@@ -248,7 +264,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
 }
 
 // ---- the threads that issue the products -----------------------------------------------------------
-enum Product { kLogits, kResults, kSums };
+enum Product { kLogits, kResults };
 template <class G, int WHICH>
 __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& sh, uint32_t ring, uint32_t q_slots, uint32_t weights,
                                          uint32_t ones, uint32_t tmem) {
@@ -273,8 +289,7 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
       if (WHICH == kLogits) {
         if (!wait(&sh.full[slot], phase) || !wait(&sh.s_free[buf], (u >> 1 & 1) ^ 1)) return;
       } else {
-        if (WHICH == kResults && !wait(&sh.full[slot], phase)) return;
-        if (!wait(&sh.p_full[pb], u / G::kPBuffers & 1)) return;
+        if (!wait(&sh.full[slot], phase) || !wait(&sh.p_full[pb], u / G::kPBuffers & 1)) return;
       }
       fence_to_tensor_cores();
       tc_fence_after_sync();
@@ -291,14 +306,12 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
         const uint32_t w = weights + pb * G::kPBytes, values = ring + slot * G::kSlot;
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks) {
-          const uint64_t b = desc_rows(w + ks / 4 * G::kQBlock + ks % 4 * 32, 1024);
-          if (WHICH == kResults)
-            mma_ss(tmem + 2 * N, desc_columns(values + ks * 2048, G::kHalves == 2 ? kBlock : 0), b, kColumnsDesc, i || ks ? 1 : 0);
-          else
-            mma_ss(tmem + 3 * N, desc_rows(ones, 0), b, kRowsDesc, i || ks ? 1 : 0);
+          const uint32_t v = values + ks * 2048;
+          mma_ss(tmem + 2 * N, desc_columns(v, G::kSumRows ? ones - v : kBlock), desc_rows(w + ks / 4 * G::kQBlock + ks % 4 * 32, 1024),
+                 kColumnsDesc, i || ks ? 1 : 0);
         }
         tc_commit(&sh.p_done[pb]);
-        if (WHICH == kResults) tc_commit(&sh.empty[slot]);
+        tc_commit(&sh.empty[slot]);
       }
       slot += 2;
       if (slot >= G::kSlots) {
@@ -318,7 +331,7 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
 // they compute of a segment whose copies did not come is thrown away with the call.
 template <class G>
 __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh, uint32_t ring, uint32_t weights, uint32_t tmem) {
-  constexpr int N = G::N, DP = G::DP, kMine = G::kMine, kChunk = G::kChunk;
+  constexpr int N = G::N, DP = G::DP, kMine = G::kMine;
   const KvCacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int key = tid & 127, half = tid >> 7, mine = half * kMine;  // this thread's key, and the first of its rows
@@ -344,125 +357,112 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     if (nt == 0) return;
     const Visible sees = visible(p, x);
     const bool several = x.n > 1;
-    for (int r = mine + key; r < mine + kMine; r += 128) {
-      sh.largest[r] = kNone;
-      sh.base[r] = 0.f;
-      sh.high[r] = several ? x.base_high + (x.row0 + min(r, rows - 1)) / p.group : x.base_high;
+    const int one_high = x.base_high;
+    if (several) {
+      for (int r = mine + key; r < mine + kMine; r += 128) sh.high[r] = x.base_high + (x.row0 + min(r, rows - 1)) / p.group;
+      meet_half();
     }
-    meet_half();
     bool fresh = true;  // some row has not seen a key yet
+    float l[kMine];     // (kSumRows: not used)
+#pragma unroll
+    for (int r = 0; r < kMine; ++r) l[r] = 0.f;
 
 #pragma unroll 1
     for (int i = 0; i < nt; ++i, ++u) {
       const uint32_t buf = u & 1, pb = u % G::kPBuffers;
       const int pos0 = (x.tile + i) * kTile, pos = pos0 + key;
       const bool all = pos0 >= sees.low_max && pos0 + kTile <= sees.high_min;
-      const uint32_t logits = lanes + buf * N + mine, w_to = weights + pb * G::kPBytes + w_key;
+      const uint32_t w_to = weights + pb * G::kPBytes + w_key;
       wait(&sh.s_full[buf], u >> 1 & 1);
       tc_fence_after_sync();
-      auto seen = [&](int r) {
-        const int high = sh.high[mine + r];
-        return all || (pos < high && !(p.window && pos < high - p.window));
-      };
-      if (i == 0) {  // bases to begin with: the largest logit of a row over the 32 keys of one warp, a quarter of the rows each
-#pragma unroll 1
-        for (int c0 = 0; c0 < kMine; c0 += kChunk) {
-          float y[kChunk];
-          load_columns(logits + c0, y);
-          tc_wait_ld();
+      float y[kMine];  // logits in units of log2; -inf where the row does not see the key
+      load_columns(lanes + buf * N + mine, y);
+      tc_wait_ld();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.s_free[buf]);
 #pragma unroll
-          for (int r = 0; r < kChunk; r += 4) {
-            // (row r + warp % 4, without an index that is not known to the compiler)
-            const float z = (warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]);
-            const int row = c0 + r + (warp & 3);
-            const float top = warp_max(seen(row) ? z * p.scale_log2 : kNone);
-            if (lane == 0) {
-              sh.largest[mine + row] = top;
-              sh.base[mine + row] = top == kNone ? 0.f : top;
-            }
-          }
+      for (int r = 0; r < kMine; ++r) y[r] *= p.scale_log2;
+      if (!all) {
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) {
+          const int high = several ? sh.high[mine + r] : one_high;
+          if (pos >= high || (p.window && pos < high - p.window)) y[r] = kNone;
         }
-        meet_half();
-        bool none = false;
-        for (int r = lane; r < kMine; r += 32) none |= *(volatile float*)&sh.largest[mine + r] == kNone;
-        fresh = __any_sync(~0u, none);
       }
-      wait(&sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1);  // (the weights that were there are multiplied)
-
-      // weights relative to the bases as they are; `over`: some logit is too far above its base (or there is none yet), and
-      // all of it is done again
-      bool over = fresh;
-      auto weigh = [&](bool look) {
-#pragma unroll 1
-        for (int c0 = 0; c0 < kMine; c0 += kChunk) {
-          float y[kChunk];
-          load_columns(logits + c0, y);
-          tc_wait_ld();
+      if (i == 0) {  // bases to begin with: the largest logit of a row over the 32 keys of one warp, a quarter of the rows each
+        bool none = false;
 #pragma unroll
-          for (int r = 0; r < kChunk; r += 4) {
-            const float4 base = *reinterpret_cast<const float4*>(&sh.base[mine + c0 + r]);
-            y[r] = fmaf(y[r], p.scale_log2, -base.x);
-            y[r + 1] = fmaf(y[r + 1], p.scale_log2, -base.y);
-            y[r + 2] = fmaf(y[r + 2], p.scale_log2, -base.z);
-            y[r + 3] = fmaf(y[r + 3], p.scale_log2, -base.w);
+        for (int r = 0; r < kMine; r += 4) {
+          // (row r + warp % 4, without an index that is not known to the compiler)
+          const float top = warp_max((warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]));
+          none |= top == kNone;
+          if (lane == 0) {
+            sh.largest[mine + r + (warp & 3)] = top;
+            sh.base[mine + r + (warp & 3)] = top == kNone ? 0.f : top;
           }
-          if (!all) {
-#pragma unroll
-            for (int r = 0; r < kChunk; ++r)
-              if (!seen(c0 + r)) y[r] = kNone;
-          }
-          if (look) {
-#pragma unroll
-            for (int r = 0; r < kChunk; ++r) over |= y[r] > kSlack;
-          }
-#pragma unroll
-          for (int r = 0; r < kChunk; ++r) store_half(w_to + (c0 + r) * 128 + (w_vec ^ (r & 7)) * 16, exp2_fast(y[r]));
         }
-      };
-      weigh(true);
-      over = any_of(1 + half, 128, over);
-      if (over) {  // move the bases: the largest logit of every row over the 128 keys
-#pragma unroll 1
-        for (int c0 = 0; c0 < kMine; c0 += kChunk) {
-          float y[kChunk];
-          load_columns(logits + c0, y);
-          tc_wait_ld();
+        fresh = any_of(1 + half, 128, none);
+      }
+      bool over = fresh;  // some logit is too far above its base, or there is none yet
+      float4 base[kMine / 4];
 #pragma unroll
-          for (int r = 0; r < kChunk; ++r) {
-            const float top = warp_max(seen(c0 + r) ? y[r] * p.scale_log2 : kNone);
-            if (lane == 0) sh.tops[warp & 3][mine + c0 + r] = top;
-          }
+      for (int r = 0; r < kMine / 4; ++r) base[r] = *reinterpret_cast<const float4*>(&sh.base[mine + 4 * r]);
+#pragma unroll
+      for (int r = 0; r < kMine; ++r) {
+        const float4 b = base[r / 4];
+        y[r] -= r % 4 == 0 ? b.x : r % 4 == 1 ? b.y : r % 4 == 2 ? b.z : b.w;
+        over |= y[r] > kSlack;
+      }
+      if (any_of(1 + half, 128, over)) {  // move the bases: the largest logit of every row over the 128 keys
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) {
+          const float top = warp_max(y[r]);
+          if (lane == 0) sh.tops[warp & 3][mine + r] = top;
         }
         meet_half();
         for (int r = mine + key; r < mine + kMine; r += 128) {
-          const float old = sh.largest[r];
-          const float now = fmaxf(fmaxf(fmaxf(old, sh.tops[0][r]), fmaxf(sh.tops[1][r], sh.tops[2][r])), sh.tops[3][r]);
-          const float base = now == kNone ? 0.f : now;
-          sh.alpha[r] = exp2_fast(old - base);
+          const float old = sh.largest[r], from = sh.base[r];
+          const float top = fmaxf(fmaxf(sh.tops[0][r], sh.tops[1][r]), fmaxf(sh.tops[2][r], sh.tops[3][r])) + from;
+          const float now = fmaxf(old, top), to = now == kNone ? 0.f : now;
+          sh.alpha[r] = exp2_fast(old - to);
+          sh.tops[0][r] = from - to;
           sh.largest[r] = now;
-          sh.base[r] = base;
+          sh.base[r] = to;
         }
         meet_half();
         bool none = false;
-        for (int r = lane; r < kMine; r += 32) none |= *(volatile float*)&sh.largest[mine + r] == kNone;
-        fresh = __any_sync(~0u, none);
+#pragma unroll
+        for (int r = 0; r < kMine; ++r) {
+          y[r] += sh.tops[0][mine + r];
+          if (!G::kSumRows) l[r] *= i ? sh.alpha[mine + r] : 1.f;
+          none |= sh.largest[mine + r] == kNone;
+        }
+        fresh = none;  // (the same for all of them)
         if (i > 0) {  // the sums so far, when the products that add to them are done
           const uint32_t before = u - 1;
           wait(&sh.p_done[before % G::kPBuffers], before / G::kPBuffers & 1);
           tc_fence_after_sync();
+          float z[8];
 #pragma unroll 1
-          for (int c0 = 0; c0 < 2 * kMine; c0 += kChunk) {
-            const uint32_t sums = lanes + (c0 < kMine ? 2 * N : 3 * N - kMine) + mine + c0;
-            float y[kChunk];
-            load_columns(sums, y);
+          for (int r0 = 0; r0 < kMine; r0 += 8) {
+            load_columns(lanes + 2 * N + mine + r0, z);
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < kChunk; ++r) y[r] *= sh.alpha[mine + c0 % kMine + r];
-            store_columns(sums, y);
+            for (int r = 0; r < 8; ++r) z[r] *= sh.alpha[mine + r0 + r];
+            store_columns(lanes + 2 * N + mine + r0, z);
           }
           tc_wait_st();
         }
-        weigh(false);
+        meet_half();  // (alpha and tops are free again)
+      }
+      // weights, rounded to fp16 for the product (2^-11 of each at most, or 2^-25 of the largest)
+      wait(&sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1);  // (those that were there are multiplied)
+#pragma unroll
+      for (int r = 0; r < kMine; ++r) {
+        const float w = exp2_fast(y[r]);
+        if (!G::kSumRows) l[r] += w;
+        store_half(w_to + r * 128 + (w_vec ^ (r & 7)) * 16, w);
       }
       tc_fence_before_sync();
       if (several && !all && half == 0) {  // values of keys that not every row sees: what is not finite is left out
@@ -478,60 +478,75 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       }
       fence_to_tensor_cores();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&sh.s_free[buf]);
-        mbar_arrive(&sh.p_full[pb]);
-      }
+      if (lane == 0) mbar_arrive(&sh.p_full[pb]);
     }
 
-    // ---- results: lane d has element d of all rows
+    // ---- results: lane d has element d of all rows; the sums of the weights go to tops[0]
+    if (!G::kSumRows) {
+#pragma unroll
+      for (int r = 0; r < kMine; ++r) {
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) l[r] += __shfl_xor_sync(~0u, l[r], d);
+        if (lane == 0) sh.tops[warp & 3][mine + r] = l[r];
+      }
+    }
     const uint32_t last = u - 1;
     wait(&sh.p_done[last % G::kPBuffers], last / G::kPBuffers & 1);
     tc_fence_after_sync();
-    if (several) meet();
+    if (G::kSumRows && (warp & 3) == 2) {  // (lanes 64 - 127 all have them)
+      float z[kMine];
+      load_columns(lanes + 2 * N + mine, z);
+      tc_wait_ld();
+#pragma unroll
+      for (int r = 0; r < kMine; ++r)
+        if (lane == 0) sh.tops[0][mine + r] = z[r];
+    }
+    meet();
+    auto sum_of = [&](int r) {
+      return G::kSumRows ? sh.tops[0][r] : (sh.tops[0][r] + sh.tops[1][r]) + (sh.tops[2][r] + sh.tops[3][r]);
+    };
     if (tid == 0) sh.not_finite[odd ^ 1] = 0;
     const bool whole = x.c0 == x.c1;
     constexpr int kLine = part_line(DP);
-    auto give = [&](int r, int token, int head, float z, float l) {
-      if (whole) {
-        uint16_t* to = p.out + ((long long)(x.first + token) * p.q_heads + x.h * p.group + head) * c.head_dim;
-        const __half h = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z, l));
-        if (key < c.head_dim) to[key] = *reinterpret_cast<const uint16_t*>(&h);
-      } else {
-        float* to = part_of(p, x, blockIdx.x, N, DP) + r * kLine;
-        if (key < DP) to[key] = z;
-        if (key == 0) *reinterpret_cast<float2*>(to + DP) = make_float2(sh.largest[r], l);
-      }
-    };
+    // row after row: its token and its head of the group, and where it goes
     int token = (x.row0 + mine) / p.group, head = x.row0 + mine - token * p.group;
-    if (several && *(volatile int*)&sh.not_finite[odd]) {  // (one column at a time, with what was left out)
-#pragma unroll 1
-      for (int r = mine; r < min(rows, mine + kMine); ++r) {
-        float z, l;
-        load_column(lanes + 2 * N + r, z);
-        load_column(lanes + 3 * N + r, l);
-        tc_wait_ld();
-        give(r, token, head, z + not_finite_sum<false>(p, x, sees, kTile, r, key), l);
+    uint16_t* to_out = p.out + ((long long)(x.first + token) * p.q_heads + x.h * p.group + head) * c.head_dim + key;
+    float* to_part = part_of(p, x, blockIdx.x, N, DP) + mine * kLine;
+    const int next_token = (p.q_heads - p.group) * c.head_dim;
+    auto give = [&](int r, float z) {
+      const float l = sum_of(r);
+      if (whole) {
+        const __half y = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z, l));
+        if (key < c.head_dim) *to_out = *reinterpret_cast<const uint16_t*>(&y);
+        to_out += c.head_dim;
         if (++head == p.group) {
           head = 0;
           ++token;
+          to_out += next_token;
         }
+      } else {
+        if (key < DP) to_part[key] = z;
+        if (key == 0) *reinterpret_cast<float2*>(to_part + DP) = make_float2(sh.largest[r], l);
+        to_part += kLine;
+      }
+    };
+    if (several && *(volatile int*)&sh.not_finite[odd]) {  // (one column at a time, with what was left out)
+#pragma unroll 1
+      for (int r = mine; r < min(rows, mine + kMine); ++r) {
+        float z;
+        load_column(lanes + 2 * N + r, z);
+        tc_wait_ld();
+        give(r, z + not_finite_sum<false>(p, x, sees, kTile, r, key));
       }
     } else {
 #pragma unroll 1
-      for (int c0 = mine; c0 < min(rows, mine + kMine); c0 += kChunk) {
-        float y[kChunk], l[kChunk];
-        load_columns(lanes + 2 * N + c0, y);
-        load_columns(lanes + 3 * N + c0, l);
+      for (int r0 = mine; r0 < min(rows, mine + kMine); r0 += 8) {
+        float z[8];
+        load_columns(lanes + 2 * N + r0, z);
         tc_wait_ld();
 #pragma unroll
-        for (int r = 0; r < kChunk; ++r) {
-          if (c0 + r < rows) give(c0 + r, token, head, y[r], l[r]);
-          if (++head == p.group) {
-            head = 0;
-            ++token;
-          }
-        }
+        for (int r = 0; r < 8; ++r)
+          if (r0 + r < rows) give(r0 + r, z[r]);
       }
     }
     tc_fence_before_sync();
@@ -569,15 +584,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
     }
     for (int i = 0; i < G::kPBuffers; ++i) {
       mbar_init(&sh.p_full[i], kSoftmaxWarps);
-      mbar_init(&sh.p_done[i], 2);
+      mbar_init(&sh.p_done[i], 1);
     }
     sh.abort = 0;
     sh.not_finite[0] = sh.not_finite[1] = 0;
   }
-  if (threadIdx.x < G::kOnes / 16) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ones + threadIdx.x * 16), "r"(0x3c003c00u) : "memory");
-    fence_to_tensor_cores();
-  }
+  for (int i = threadIdx.x; i < G::kOnes / 16; i += kThreads)
+    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ones + i * 16), "r"(0x3c003c00u) : "memory");
+  if (G::kSumRows) fence_to_tensor_cores();
   if (warp == kThreads / 32 - 1) {
     tmem_alloc(&sh.tmem, G::kColumns);
     tmem_relinquish();
@@ -595,10 +609,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   } else if (threadIdx.x % 32 == 0) {
     if (warp == kSoftmaxWarps + kProducers)
       multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
-    else if (warp == kSoftmaxWarps + kProducers + 1)
-      multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
     else
-      multiply<G, kSums>(p, sh, ring, q_slots, weights, ones, tmem);
+      multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
   }
   __syncwarp();
   tc_fence_before_sync();
@@ -619,8 +631,7 @@ cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t str
   const long long rows = usual_rows(p);
   if (rows <= 16) return launch<DP, 16>(p, sm_count, stream);
   if (rows <= 32) return launch<DP, 32>(p, sm_count, stream);
-  if (rows <= 64) return launch<DP, 64>(p, sm_count, stream);
-  return launch<DP, 128>(p, sm_count, stream);
+  return launch<DP, 64>(p, sm_count, stream);
 }
 
 }  // namespace
