@@ -13,9 +13,9 @@
 // 64 KB, which takes 2800 to come from memory.  (A third product, of ones with the weights, cost as much as either of the two.)
 //
 // Warps: 0 - 7 softmax and results (lane quarter w % 4 of tensor memory; 0 - 3 the first half of the rows, 4 - 7 the second, each
-// half with bases of its own), 8 - 11 copies (32 keys of every tile each), 12 and 13 issue a product each: an issue costs its thread
-// some 75 cycles and a commit 125, and with one thread for all of them everybody waited for it.
-// Keys and values take slots of the ring in turn.  Tensor memory: S twice, and O; N columns each.
+// half with bases of its own), 8 and 9 copy keys, 10 and 11 values (half of every tile each), 12 and 13 issue a product each: an issue
+// costs its thread some 75 cycles and a commit 125, and with one thread for all of them everybody waited for it.
+// Keys and values have rings of their own: values are held until the weights of their keys are there, and keys need not wait for that.  Tensor memory: S twice, and O; N columns each.
 #include "attention.cuh"
 #include "tc_utils.cuh"
 
@@ -23,13 +23,14 @@ namespace marlin_b200 {
 namespace {
 
 constexpr int kTile = 128;
-constexpr int kLead = 1;                 // what an item costs beside its tiles, in tiles
+constexpr int kLead = 4;                 // what an item costs beside its tiles, in tiles
 constexpr int kBlock = kTile * 128;      // 64 elements of the keys of a tile: rows of 128 bytes, as the swizzle has them
 constexpr int kSoftmaxWarps = 8;
 constexpr int kSoftmaxThreads = kSoftmaxWarps * 32;
 constexpr int kProducers = 4;
 constexpr int kIssuers = 2;
-constexpr int kThreads = kSoftmaxThreads + (kProducers + kIssuers) * 32;
+constexpr int kThreads = 512;  // (two warps do nothing: registers are shared out by groups of four)
+static_assert(kSoftmaxThreads + (kProducers + kIssuers) * 32 <= kThreads, "warps");
 
 // DP: head_dim rounded up to 64 or 128; N: rows of a block, 16, 32 or 64
 template <int DP_, int N_>
@@ -40,21 +41,26 @@ struct TcGeometry {
   static constexpr int kQBlock = N * 128;          // 64 elements of the rows
   static constexpr int kQBytes = kHalves * kQBlock;
   static constexpr int kOpen = 2;                  // segments that can be open at a time
-  static constexpr int kPBytes = 2 * kQBlock;      // weights: 64 keys of the rows, twice
+  static constexpr int kPRow = 2 * N;              // weights: bytes of a key, swizzled over as many
+  static constexpr int kPBytes = kTile * kPRow;
   static constexpr int kPBuffers = 2;
   static constexpr bool kSumRows = DP == 64;       // the weights are summed in the product
   static constexpr int kOnes = kSumRows ? 2048 : 0;  // 16 rows of 64 ones, beside the values of 16 keys
   static constexpr int kRest = kOpen * kQBytes + kPBuffers * kPBytes + kOnes;
   static constexpr int kSlots = (222 * 1024 - kRest) / kSlot > 12 ? 12 : (222 * 1024 - kRest) / kSlot;
+  static constexpr int kKeySlots = kSlots / 2, kValueSlots = kSlots - kKeySlots;
+  // registers a thread where the launch's 128 are too few for the softmax warps (64 rows)
+  static constexpr int kSoftmaxRegs = N == 64 ? 160 : 0, kOtherRegs = 96;
+  static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "registers");
   static constexpr int kSmem = kSlots * kSlot + kRest + 1024;  // (the ring begins at a multiple of 1024)
   static constexpr int kColumns = 4 * N;           // of tensor memory: S, S, O, and N that a power of two brings along
   static constexpr int kMine = N / 2;              // rows of a half of the softmax warps
-  static_assert(kSlots >= 3 && kColumns <= 512, "ring");
+  static_assert(kKeySlots >= 2 && kColumns <= 512, "ring");
 };
 
 template <class G>
 struct TcShared {
-  uint64_t full[G::kSlots], empty[G::kSlots];
+  uint64_t full[G::kSlots], empty[G::kSlots];  // keys, then values
   uint64_t opened[G::kOpen], closed[G::kOpen];
   uint64_t s_full[2], s_free[2];                       // logits are there; have been read
   uint64_t p_full[G::kPBuffers], p_done[G::kPBuffers]; // weights are there; have been multiplied
@@ -81,6 +87,17 @@ __device__ __forceinline__ uint64_t desc_columns(uint32_t addr, uint32_t block) 
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
          ((uint64_t)2 << 61);
 }
+// the same along rows of 128, 64 or 32 bytes that are one block, swizzled over their length: modes 2, 4, 6; eight rows lie together
+template <int ROW>
+__device__ __forceinline__ uint64_t desc_weights(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(8 * ROW >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)(ROW == 128 ? 2 : ROW == 64 ? 4 : 6) << 61);
+}
+// what the 16-byte vectors of row `key` are permuted by
+template <int ROW>
+__device__ __forceinline__ int swizzle_of(int key) {
+  return ROW == 128 ? key & 7 : ROW == 64 ? key >> 1 & 3 : key >> 2 & 1;
+}
 // D[tmem] (+)= A[smem] . B[smem]
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -94,10 +111,6 @@ __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_
 }
 // what this thread (or another whose arrival it has seen) wrote to shared memory can be read by the tensor cores
 __device__ __forceinline__ void fence_to_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void store_half(uint32_t addr, float x) {
-  const __half h = __float2half_rn(x);
-  asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(*reinterpret_cast<const uint16_t*>(&h)) : "memory");
-}
 __device__ __forceinline__ float warp_max(float x) {
   float y;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -152,10 +165,11 @@ __device__ __forceinline__ bool arrived_at(TcShared<G>& sh, uint64_t* bar, uint3
 }
 
 // ---- the warps that copy ---------------------------------------------------------------------------
+// `values`: these, not keys; `upper`: the second half of every tile
 template <class G>
-__device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& sh, int producer, uint32_t ring, uint32_t q_slots) {
+__device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& sh, bool values, bool upper, uint32_t ring, uint32_t q_slots) {
   const KvCacheView& c = p.cache;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, producer = 2 * values + upper;
   Range<G::N, kTile, kLead> range;
   range.begin(p);
 
@@ -164,8 +178,10 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
   const int my_row = lane / kVectors, my_vec = lane % kVectors;
   const bool my_part = my_vec * 8 < c.head_dim;
   const bool big_pages = c.page_shift >= 4;  // sixteen keys lie in one page
-  const long long values_off = static_cast<const uint8_t*>(c.v) - static_cast<const uint8_t*>(c.k);
-  int slot = 0, open = 0;
+  const uint8_t* const cache = static_cast<const uint8_t*>(values ? c.v : c.k);
+  const long long pass = my_part ? kPer * c.s_token * 2 : 0;
+  const int first_slot = values ? G::kKeySlots : 0, last_slot = values ? G::kSlots - 1 : G::kKeySlots - 1;
+  int slot = first_slot, open = 0;
   uint32_t slot_phase = 1, open_phase = 1;
 #pragma unroll 1
   for (;;) {
@@ -192,70 +208,57 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
 
     const Visible v = visible(p, x);
     const int* const table = c.table + x.b * c.table_stride;
-    const int key_first = x.tile * kTile + producer * 32;
+    const int key_first = x.tile * kTile + upper * 64;
     const int low = max(v.low_min, x.tile * kTile), high = min(v.high_max, (x.tile + x.nt) * kTile);
-    // pages: of the two sixteens of this warp in sixteen tiles, a lane each, and in the next sixteen; or, where pages are smaller,
-    // of the 32 keys of one tile and of the next one.  INT_MIN where no key is asked for
+    // pages of the four sixteens of this warp in eight tiles, a lane each, and in the next eight; INT_MIN where no key is asked for
     auto page_of = [&](int i) {
-      const int key = key_first + (big_pages ? (i + lane / 2) * kTile + lane % 2 * 16 : i * kTile + lane);
-      return key < high && key + (big_pages ? 16 : 1) > low ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
+      const int key = key_first + (i + lane / 4) * kTile + lane % 4 * 16;
+      return big_pages && key < high && key + 16 > low ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
     };
-    const int batch = big_pages ? 16 : 1;
     const long long head_bytes = (x.h * c.s_head + my_row * c.s_token) * 2 + my_vec * 16;
-    const long long pass = my_part ? kPer * c.s_token * 2 : 0;
-    int pages = page_of(0), pages_next = page_of(batch), in_batch = 0;
+    int pages = page_of(0), pages_next = page_of(8), in_batch = 0;
     bool go_on = true;
 #pragma unroll 1
-    for (int i = 0; i < x.nt && go_on; ++i, ++in_batch) {
-      if (in_batch == batch) {
+    for (int i = 0; i < x.nt; ++i, ++in_batch) {
+      if (in_batch == 8) {
         in_batch = 0;
         pages = pages_next;
-        pages_next = page_of(i + batch);
+        pages_next = page_of(i + 8);
       }
-      // the two sixteens of this warp: where they begin in the cache, or that some key of them is not there
       const int key0 = key_first + i * kTile;
-      const uint8_t* from[2];
-      bool whole = big_pages && key0 >= low && key0 + 32 <= high;
+      const bool there4 = lane / 4 != in_batch || (unsigned)pages < (unsigned)c.pages;
+      const bool whole = big_pages && key0 >= low && key0 + 64 <= high && __all_sync(~0u, there4);
+      go_on = arrived_at(sh, &sh.empty[slot], slot_phase, p.status);
+      if (!go_on) break;
+      const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (upper * 64 + my_row) * 128;
+      if (whole) {
+#pragma unroll 2
+        for (int j = 0; j < 4; ++j) {
+          const int page = __shfl_sync(~0u, pages, in_batch * 4 + j);
+          const uint8_t* src = cache;
+          if (my_part) src += (page * c.s_page + ((key0 + j * 16) & ((1 << c.page_shift) - 1)) * c.s_token) * 2 + head_bytes;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int page = __shfl_sync(~0u, pages, big_pages ? in_batch * 2 + j : 0);
-        whole = whole && (unsigned)page < (unsigned)c.pages;
-        const long long first = (page * c.s_page + ((key0 + j * 16) & ((1 << c.page_shift) - 1)) * c.s_token) * 2 + head_bytes;
-        from[j] = static_cast<const uint8_t*>(c.k) + (whole && my_part ? first : 0);
+          for (int r = 0; r < 16; r += kPer) {
+            copy16(to + (j * 16 + r) * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
+            src += pass;
+          }
+        }
+      } else {  // pages smaller than that, the ends of a sequence, pages that are not there
+#pragma unroll 4
+        for (int r = 0; r < 64; r += kPer) {
+          const int row = r + my_row, key = key0 + row;
+          const bool asked = key >= low && key < high;
+          const long long at = asked ? cache_offset(c, __ldg(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
+          const bool there = at >= 0 && my_part;
+          copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
+        }
       }
-#pragma unroll 1
-      for (int which = 0; which < 2; ++which) {  // keys, values
-        if (!arrived_at(sh, &sh.empty[slot], slot_phase, p.status)) {
-          go_on = false;
-          break;
-        }
-        const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (producer * 32 + my_row) * 128;
-        if (whole) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint8_t* src = from[j] + (which ? values_off : 0);
-#pragma unroll
-            for (int r = 0; r < 16; r += kPer) {
-              copy16(to + (j * 16 + r) * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
-              src += pass;
-            }
-          }
-        } else {
-          const uint8_t* const cache = static_cast<const uint8_t*>(which ? c.v : c.k);
-#pragma unroll 1
-          for (int r = 0; r < 32; r += kPer) {
-            const int row = r + my_row, key = key0 + row;
-            const int mine = __shfl_sync(~0u, pages, big_pages ? in_batch * 2 + row / 16 : row);
-            const long long at = key >= low && key < high ? cache_offset(c, mine, x.h, key, p.status) : -1;
-            const bool there = at >= 0 && my_part;
-            copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
-          }
-        }
-        copies_arrive(&sh.full[slot]);
-        if (++slot == G::kSlots) {
-          slot = 0;
-          slot_phase ^= 1;
-        }
+      copies_arrive(&sh.full[slot]);
+      if (slot == last_slot) {
+        slot = first_slot;
+        slot_phase ^= 1;
+      } else {
+        ++slot;
       }
     }
     if (!go_on) break;
@@ -270,12 +273,13 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
                                          uint32_t ones, uint32_t tmem) {
   constexpr int N = G::N;
   constexpr uint32_t kRowsDesc = instr_desc_f16(128, N);
-  constexpr uint32_t kColumnsDesc = kRowsDesc | 1u << 15;  // A along its bytes
+  constexpr uint32_t kColumnsDesc = kRowsDesc | 1u << 15 | 1u << 16;  // A and B along their bytes
   auto wait = [&](uint64_t* bar, uint32_t parity) {
     mbar_wait(bar, parity, &sh.abort, p.status);
     return *(volatile int*)&sh.abort == 0;
   };
-  int slot = WHICH == kLogits ? 0 : 1, open = 0;  // slots go round: keys of tile u, values of tile u
+  constexpr int kFirst = WHICH == kLogits ? 0 : G::kKeySlots, kLast = WHICH == kLogits ? G::kKeySlots - 1 : G::kSlots - 1;
+  int slot = kFirst, open = 0;
   uint32_t phase = 0, open_phase = 0, u = 0;
 #pragma unroll 1
   for (;;) {
@@ -307,16 +311,17 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks) {
           const uint32_t v = values + ks * 2048;
-          mma_ss(tmem + 2 * N, desc_columns(v, G::kSumRows ? ones - v : kBlock), desc_rows(w + ks / 4 * G::kQBlock + ks % 4 * 32, 1024),
+          mma_ss(tmem + 2 * N, desc_columns(v, G::kSumRows ? ones - v : kBlock), desc_weights<G::kPRow>(w + ks * 16 * G::kPRow),
                  kColumnsDesc, i || ks ? 1 : 0);
         }
         tc_commit(&sh.p_done[pb]);
         tc_commit(&sh.empty[slot]);
       }
-      slot += 2;
-      if (slot >= G::kSlots) {
-        slot -= G::kSlots;
+      if (slot == kLast) {
+        slot = kFirst;
         phase ^= 1;
+      } else {
+        ++slot;
       }
     }
     if (++open == G::kOpen) {
@@ -346,8 +351,6 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
   uint32_t u = 0;  // tiles so far
   int open = 0, odd = 0;
   uint32_t open_phase = 0;
-  // where this thread's key lies in the weights: byte of row r = w_key + r * 128, with the 16-byte vectors of a row permuted by r
-  const uint32_t w_key = key / 64 * G::kQBlock + key % 8 * 2 + mine * 128, w_vec = key % 64 / 8;
 #pragma unroll 1
   for (;; odd ^= 1) {
     wait(&sh.opened[open], open_phase);
@@ -363,6 +366,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       meet_half();
     }
     bool fresh = true;  // some row has not seen a key yet
+    const float hidden = p.scale_log2 < 0.f ? INFINITY : -INFINITY;
     float l[kMine];     // (kSumRows: not used)
 #pragma unroll
     for (int r = 0; r < kMine; ++r) l[r] = 0.f;
@@ -372,22 +376,19 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       const uint32_t buf = u & 1, pb = u % G::kPBuffers;
       const int pos0 = (x.tile + i) * kTile, pos = pos0 + key;
       const bool all = pos0 >= sees.low_max && pos0 + kTile <= sees.high_min;
-      const uint32_t w_to = weights + pb * G::kPBytes + w_key;
       wait(&sh.s_full[buf], u >> 1 & 1);
       tc_fence_after_sync();
-      float y[kMine];  // logits in units of log2; -inf where the row does not see the key
+      float y[kMine];
       load_columns(lanes + buf * N + mine, y);
       tc_wait_ld();
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.s_free[buf]);
-#pragma unroll
-      for (int r = 0; r < kMine; ++r) y[r] *= p.scale_log2;
-      if (!all) {
+      if (!all) {  // (a logit that becomes -inf whatever it is multiplied with)
 #pragma unroll
         for (int r = 0; r < kMine; ++r) {
           const int high = several ? sh.high[mine + r] : one_high;
-          if (pos >= high || (p.window && pos < high - p.window)) y[r] = kNone;
+          if (pos >= high || (p.window && pos < high - p.window)) y[r] = hidden;
         }
       }
       if (i == 0) {  // bases to begin with: the largest logit of a row over the 32 keys of one warp, a quarter of the rows each
@@ -395,7 +396,8 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
 #pragma unroll
         for (int r = 0; r < kMine; r += 4) {
           // (row r + warp % 4, without an index that is not known to the compiler)
-          const float top = warp_max((warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]));
+          const float z = (warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]);
+          const float top = warp_max(z == hidden ? kNone : z * p.scale_log2);
           none |= top == kNone;
           if (lane == 0) {
             sh.largest[mine + r + (warp & 3)] = top;
@@ -404,16 +406,18 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         }
         fresh = any_of(1 + half, 128, none);
       }
-      bool over = fresh;  // some logit is too far above its base, or there is none yet
-      float4 base[kMine / 4];
+      // logits in units of log2, relative to the bases; `over`: some are too far above, or there is no base yet
+      float top = kNone;
 #pragma unroll
-      for (int r = 0; r < kMine / 4; ++r) base[r] = *reinterpret_cast<const float4*>(&sh.base[mine + 4 * r]);
-#pragma unroll
-      for (int r = 0; r < kMine; ++r) {
-        const float4 b = base[r / 4];
-        y[r] -= r % 4 == 0 ? b.x : r % 4 == 1 ? b.y : r % 4 == 2 ? b.z : b.w;
-        over |= y[r] > kSlack;
+      for (int r = 0; r < kMine; r += 4) {
+        const float4 base = *reinterpret_cast<const float4*>(&sh.base[mine + r]);
+        y[r] = fmaf(y[r], p.scale_log2, -base.x);
+        y[r + 1] = fmaf(y[r + 1], p.scale_log2, -base.y);
+        y[r + 2] = fmaf(y[r + 2], p.scale_log2, -base.z);
+        y[r + 3] = fmaf(y[r + 3], p.scale_log2, -base.w);
+        top = fmaxf(fmaxf(fmaxf(top, y[r]), fmaxf(y[r + 1], y[r + 2])), y[r + 3]);
       }
+      const bool over = fresh || top > kSlack;
       if (any_of(1 + half, 128, over)) {  // move the bases: the largest logit of every row over the 128 keys
 #pragma unroll
         for (int r = 0; r < kMine; ++r) {
@@ -458,16 +462,27 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       }
       // weights, rounded to fp16 for the product (2^-11 of each at most, or 2^-25 of the largest)
       wait(&sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1);  // (those that were there are multiplied)
+      const uint32_t w_to = weights + pb * G::kPBytes + key * G::kPRow;
 #pragma unroll
-      for (int r = 0; r < kMine; ++r) {
-        const float w = exp2_fast(y[r]);
-        if (!G::kSumRows) l[r] += w;
-        store_half(w_to + r * 128 + (w_vec ^ (r & 7)) * 16, w);
+      for (int r = 0; r < kMine; r += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          y[r + e] = exp2_fast(y[r + e]);
+          y[r + e + 1] = exp2_fast(y[r + e + 1]);
+          w[e / 2] = half2_bits(y[r + e], y[r + e + 1]);
+          if (!G::kSumRows) {
+            l[r + e] += y[r + e];
+            l[r + e + 1] += y[r + e + 1];
+          }
+        }
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(w_to + (((mine + r) / 8) ^ swizzle_of<G::kPRow>(key)) * 16),
+                     "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
       }
       tc_fence_before_sync();
       if (several && !all && half == 0) {  // values of keys that not every row sees: what is not finite is left out
-        const uint32_t v_slot = (2 * u + 1) % G::kSlots;
-        wait(&sh.full[v_slot], (2 * u + 1) / G::kSlots & 1);
+        const uint32_t v_slot = G::kKeySlots + u % G::kValueSlots;
+        wait(&sh.full[v_slot], u / G::kValueSlots & 1);
         if ((pos >= sees.high_min && pos < sees.high_max) || (pos >= sees.low_min && pos < sees.low_max)) {
           bool found = false;
 #pragma unroll 1
@@ -481,14 +496,21 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       if (lane == 0) mbar_arrive(&sh.p_full[pb]);
     }
 
-    // ---- results: lane d has element d of all rows; the sums of the weights go to tops[0]
+    // ---- results: lane d has element d of all rows; the sums of the weights go to `alpha`
     if (!G::kSumRows) {
+      // lanes exchange halves of their sums until each has all of one row (of `same` lanes that end with the same one)
+      constexpr int kSame = 32 / kMine;
 #pragma unroll
-      for (int r = 0; r < kMine; ++r) {
+      for (int n = kMine / 2, bit = 16; n >= 1; n /= 2, bit /= 2) {
 #pragma unroll
-        for (int d = 1; d < 32; d *= 2) l[r] += __shfl_xor_sync(~0u, l[r], d);
-        if (lane == 0) sh.tops[warp & 3][mine + r] = l[r];
+        for (int r = 0; r < n; ++r) {
+          const float mine_of = (lane & bit) ? l[r + n] : l[r], other = (lane & bit) ? l[r] : l[r + n];
+          l[r] = mine_of + __shfl_xor_sync(~0u, other, bit);
+        }
       }
+#pragma unroll
+      for (int bit = kSame / 2; bit >= 1; bit /= 2) l[0] += __shfl_xor_sync(~0u, l[0], bit);
+      if (lane % kSame == 0) sh.tops[warp & 3][mine + lane / kSame] = l[0];
     }
     const uint32_t last = u - 1;
     wait(&sh.p_done[last % G::kPBuffers], last / G::kPBuffers & 1);
@@ -499,12 +521,13 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       tc_wait_ld();
 #pragma unroll
       for (int r = 0; r < kMine; ++r)
-        if (lane == 0) sh.tops[0][mine + r] = z[r];
+        if (lane == 0) sh.alpha[mine + r] = z[r];
     }
     meet();
-    auto sum_of = [&](int r) {
-      return G::kSumRows ? sh.tops[0][r] : (sh.tops[0][r] + sh.tops[1][r]) + (sh.tops[2][r] + sh.tops[3][r]);
-    };
+    if (!G::kSumRows) {
+      if (tid < N) sh.alpha[tid] = (sh.tops[0][tid] + sh.tops[1][tid]) + (sh.tops[2][tid] + sh.tops[3][tid]);
+      meet();
+    }
     if (tid == 0) sh.not_finite[odd ^ 1] = 0;
     const bool whole = x.c0 == x.c1;
     constexpr int kLine = part_line(DP);
@@ -514,9 +537,9 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     float* to_part = part_of(p, x, blockIdx.x, N, DP) + mine * kLine;
     const int next_token = (p.q_heads - p.group) * c.head_dim;
     auto give = [&](int r, float z) {
-      const float l = sum_of(r);
+      const float sum = sh.alpha[r];
       if (whole) {
-        const __half y = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z, l));
+        const __half y = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z, sum));
         if (key < c.head_dim) *to_out = *reinterpret_cast<const uint16_t*>(&y);
         to_out += c.head_dim;
         if (++head == p.group) {
@@ -526,7 +549,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         }
       } else {
         if (key < DP) to_part[key] = z;
-        if (key == 0) *reinterpret_cast<float2*>(to_part + DP) = make_float2(sh.largest[r], l);
+        if (key == 0) *reinterpret_cast<float2*>(to_part + DP) = make_float2(sh.largest[r], sum);
         to_part += kLine;
       }
     };
@@ -571,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   const int warp = threadIdx.x / 32;
   if (threadIdx.x == 0) {
     for (int i = 0; i < G::kSlots; ++i) {
-      mbar_init(&sh.full[i], 32 * kProducers);
+      mbar_init(&sh.full[i], 32 * kProducers / 2);
       mbar_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < G::kOpen; ++i) {
@@ -603,13 +626,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   if (warp < kSoftmaxWarps) {
+    if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_inc<G::kSoftmaxRegs>();
     soften<G>(p, sh, ring, weights, tmem);
-  } else if (warp < kSoftmaxWarps + kProducers) {
-    produce<G>(p, sh, warp - kSoftmaxWarps, ring, q_slots);
-  } else if (threadIdx.x % 32 == 0) {
-    if (warp == kSoftmaxWarps + kProducers)
+  } else {
+    if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_dec<G::kOtherRegs>();
+    const int w = warp - kSoftmaxWarps;
+    if (w < kProducers)
+      produce<G>(p, sh, w / 2, w % 2, ring, q_slots);
+    else if (w == kProducers && threadIdx.x % 32 == 0)
       multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
-    else
+    else if (w == kProducers + 1 && threadIdx.x % 32 == 0)
       multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
   }
   __syncwarp();
@@ -624,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
 template <int DP, int N>
 cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) {
   using G = TcGeometry<DP, N>;
-  return launch_ranges<attention_tc_kernel<DP, N>, G::kSmem, kThreads, N, kTile>(p, sm_count, stream);
+  return launch_ranges<attention_tc_kernel<DP, N>, G::kSmem, kThreads, N, kTile>(p, sm_count, stream, G::kSoftmaxRegs ? 128 : 0);
 }
 template <int DP>
 cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
