@@ -82,13 +82,14 @@ __device__ __forceinline__ uint32_t further(uint32_t address, int vec) {
   return (address ^ (uint32_t)(vec % kLine * 16)) + vec / kLine * (kLine * 16);
 }
 
-// Barriers and notes in shared memory.  Every wait is bounded (mbar_wait): when one runs out, `abort` is set, all warps leave at their
-// next wait, and the host finds MARLIN_ERR_DEVICE_TIMEOUT; no hardware barrier is used after the start, so none is left waiting.
+// Barriers and notes in shared memory.  Every wait for one is bounded (mbar_wait): when one runs out, `abort` is set, all others return at
+// once, and the host finds MARLIN_ERR_DEVICE_TIMEOUT.  The warps that multiply agree on that where a segment begins, so that
+// they always meet at the same hardware barriers; what they compute of a segment whose copies did not come is thrown away with
+// the call.
 template <class G>
 struct Shared {
   uint64_t full[G::kStages], empty[G::kStages];  // a stage has arrived; has been multiplied
   uint64_t opened[G::kOpen], closed[G::kOpen];   // a segment and its Q are there; nobody needs them any more
-  uint64_t meet;                                 // of the warps that multiply
   Segment segments[G::kOpen];
   float2 ml[G::kTeams * G::kRows];               // base and sum of weights of the warps' rows
   int abort;
@@ -224,12 +225,10 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
   const uint32_t k_lane = place<G::kVectors>(part * 16 + (lane & 15), lane >> 4);
   const uint32_t v_lane = F8 ? k_lane : place<G::kVectors>(part * 16 + (lane & 7) + (lane >> 4) * 8, (lane >> 3) & 1);
 
-  uint32_t meet_phase = 0;
-  auto meet = [&] {  // all warps that multiply; false: a wait ran out
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.meet);
-    meet_phase ^= 1;
-    return arrived_at(sh, &sh.meet, meet_phase ^ 1, p.status);
+  auto wait = [&](uint64_t* bar, uint32_t parity) { mbar_wait(bar, parity, &sh.abort, p.status); };
+  auto meet = [&] {  // all warps that multiply
+    named_bar_sync(1, kMine);
+    return true;
   };
 
   // the next tile of this group, in the numbering of all tiles of the CTA: its stage and phase
@@ -239,7 +238,8 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
   int slot = 0, odd = 0;
 #pragma unroll 1
   for (;; odd ^= 1) {
-    if (!arrived_at(sh, &sh.opened[slot], slot_phase, p.status)) return;
+    wait(&sh.opened[slot], slot_phase);
+    if (any_of(1, kMine, *(volatile int*)&sh.abort)) return;  // (what there was of the segment before was read as well)
     const Segment& x = sh.segments[slot];
     const int nt = x.nt, tile = x.tile, rows = x.rows;
     if (nt == 0) return;
@@ -301,7 +301,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
 
 #pragma unroll 1
     for (; next < done + nt; next += G::kGroups) {
-      if (!arrived_at(sh, &sh.full[stage], stage_phase, p.status)) return;
+      wait(&sh.full[stage], stage_phase);
       const uint32_t keys = ring + stage * G::kStage, values = keys + G::kHalf;
       // S^T = K Q^T: a thread has keys g, g + 8 of 16 and rows 2 t, 2 t + 1 of 8.  (One tile of rows alone would be a chain of
       // dependent products: it is summed in two.)
@@ -465,7 +465,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
     auto bank = [](int r, int d) { return G::kColumns >= 32 ? d ^ ((r >> 1 & 3) * 8) : d; };
 #pragma unroll
     for (int round = 0; round < G::kRounds; ++round) {
-      if (!meet()) return;  // (what was there was read)
+      if (round > 0) meet();  // (what was there was read)
       if (tid == 0 && round == 0) sh.not_finite[odd ^ 1] = 0;
 #pragma unroll
       for (int j = 0; j < NT; ++j)
@@ -482,25 +482,30 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
             }
           }
         }
-      if (!meet()) return;
+      meet();
       const bool odd_values = several && sh.not_finite[odd];
 #pragma unroll 1
       for (int i = tid; i < rows * (G::kColumns / 4); i += kMine) {
         const int r = i / (G::kColumns / 4), at_d = (i % (G::kColumns / 4)) * 4, d = round * G::kColumns + at_d;
         if (d >= c.head_dim) continue;
+        // (all of it is asked for at once: one latency, not one for each team)
+        float2 sums[G::kTeams];
+        float4 u[G::kTeams];
         float mi = kNone;
-#pragma unroll 4
-        for (int t = 0; t < G::kTeams; ++t) mi = fmaxf(mi, sh.ml[t * G::kRows + r].x);
+#pragma unroll
+        for (int t = 0; t < G::kTeams; ++t) {
+          sums[t] = sh.ml[t * G::kRows + r];
+          u[t] = *reinterpret_cast<const float4*>(join + (t * G::kRows + r) * G::kColumns + bank(r, at_d));
+          mi = fmaxf(mi, sums[t].x);
+        }
         const float base = mi == kNone ? 0.f : mi;
         float li = 0.f;
         float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll
         for (int t = 0; t < G::kTeams; ++t) {
-          const float2 sums = sh.ml[t * G::kRows + r];
-          const float f = exp2_fast(sums.x - base);
-          const float4 u = *reinterpret_cast<const float4*>(join + (t * G::kRows + r) * G::kColumns + bank(r, at_d));
-          li += sums.y * f;
-          z.x += u.x * f; z.y += u.y * f; z.z += u.z * f; z.w += u.w * f;
+          const float f = exp2_fast(sums[t].x - base);
+          li += sums[t].y * f;
+          z.x += u[t].x * f; z.y += u[t].y * f; z.z += u[t].z * f; z.w += u[t].w * f;
         }
         if (odd_values) {
 #pragma unroll 1
@@ -518,7 +523,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
         }
       }
     }
-    if (!whole && !join_parts<G::kRows, DP, kMine, 1>(p, x, tid, &sh.arrived, sh.ml, meet, write_out)) return;
+    if (!whole) join_parts<G::kRows, DP, kMine, 1>(p, x, tid, &sh.arrived, sh.ml, meet, write_out);
     __syncwarp();
     if (lane == 0) mbar_arrive(&sh.closed[slot]);
     if (++slot == G::kOpen) {
@@ -544,13 +549,13 @@ __global__ void __launch_bounds__(Geometry<DP, NT, TW, F8>::kThreads, 1) attenti
       mbar_init(&sh.opened[i], 32 * G::kProducers + 1);  // the copies of all lanes, and the note itself
       mbar_init(&sh.closed[i], G::kConsumers);
     }
-    mbar_init(&sh.meet, G::kConsumers);
     sh.abort = 0;
     sh.not_finite[0] = sh.not_finite[1] = 0;
   }
   __syncthreads();
   pdl_launch_dependents();
   pdl_wait_prior_grids();
+  prefetch_table(p, G::kThreads);
   if (threadIdx.x >= G::kConsumers * 32) {
     if constexpr (G::kProducerRegs < G::kLaunchRegs) setmaxnreg_dec<G::kProducerRegs>();
     produce<G, F8>(p, sh, (int)threadIdx.x / 32 - G::kConsumers, smem_u32(smem), ring);

@@ -6,12 +6,12 @@
 
 namespace marlin_b200 {
 
-constexpr int kLeastTiles = 2;  // tiles that a CTA takes at least, where there are fewer tiles than CTAs would like
+constexpr int kLeastTiles = 4;  // units that a CTA takes at least, where there are fewer than CTAs would like
 constexpr uint32_t kMostUnits = 1u << 30;
 constexpr int kMostCtas = kMaxWorkers;
 constexpr int kItemCounters = 2 * kMostCtas;  // counters of items behind those of groups
 static_assert(3 * kMostCtas * sizeof(int) <= kWsPartialOff - kWsCounterOff, "counters");
-constexpr int kGroup = 4;  // parts that are joined at once; more of them are joined in groups first, each by its last CTA
+constexpr int kGroup = 8;  // parts that are joined at once; more of them are joined in groups first, each by its last CTA
 constexpr float kNone = -INFINITY;
 // A row's sums are kept relative to 2^base, base its largest logit (in units of log2) when the base was last moved.  It moves only
 // when a logit exceeds it by more than this, so that most tiles neither look for a maximum across lanes nor rescale:
@@ -59,6 +59,34 @@ __device__ __forceinline__ bool clean_vector(uint32_t saddr) {
   if (found)
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
   return found;
+}
+
+// bar.sync of some warps that also tells all of them whether `mine` is set for any of their threads
+__device__ __forceinline__ bool any_of(int id, int threads, bool mine) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 p, %1, 0;\n"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"((uint32_t)mine), "r"(id), "r"(threads)
+      : "memory");
+  return r != 0;
+}
+
+// The page table is on its way to the L2 while the CTAs find their ranges: each asks for some lines of it.  (Its numbers are what the
+// first copies wait for; they come in 0.3 us then instead of 0.8.)
+__device__ __forceinline__ void prefetch_table(const AttentionParams& p, int threads) {
+  const KvCacheView& c = p.cache;
+  const long long lines = (c.sequences * c.table_stride * 4 + 127) / 128;
+  for (long long i = (long long)blockIdx.x * threads + threadIdx.x; i < lines; i += (long long)gridDim.x * threads) {
+    const long long at = i * 32;  // (a line may lie between the rows: within the table all the same, but for the end of the last row)
+    if (at < (c.sequences - 1) * c.table_stride + c.max_pages)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(c.table + at));
+  }
 }
 
 // What a sequence asks for: new tokens [first, first + n) of the call, tiles [tile0, tile0 + tiles) of its len keys, blocks of
@@ -233,23 +261,20 @@ struct Range {
   }
 };
 
+// new token of the segment's sequence that row r belongs to (a division only where there are several)
+__device__ __forceinline__ int token_of(const AttentionParams& p, const Segment& x, int r) {
+  return x.n > 1 ? (x.row0 + r) / p.group : 0;
+}
 // Row r, elements d .. d + 3 of a result: sums over the sum of the weights, zeros where the row sees nothing.
-__device__ __forceinline__ float out_factor(const AttentionParams& p, const Segment& x, int r, float li) {
-  const int token = x.n > 1 ? (x.row0 + r) / p.group : 0;
-  return x.base_high + token <= 0 ? 0.f : (p.cache.v_scale ? __ldg(p.cache.v_scale + x.h) : 1.f) / li;
-}
-__device__ __forceinline__ uint16_t* out_row(const AttentionParams& p, const Segment& x, int r) {
-  const int token = (x.row0 + r) / p.group, head = x.h * p.group + (x.row0 + r) - token * p.group;
-  return p.out + ((long long)(x.first + token) * p.q_heads + head) * p.cache.head_dim;
-}
 __device__ __forceinline__ void write_four(const AttentionParams& p, const Segment& x, int r, int d, float4 z, float li) {
-  const float f = out_factor(p, x, r, li);
-  const bool nothing = x.base_high + (x.n > 1 ? (x.row0 + r) / p.group : 0) <= 0;
+  const int token = token_of(p, x, r), head = x.h * p.group + x.row0 + r - token * p.group;
+  const bool nothing = x.base_high + token <= 0;
+  const float f = nothing ? 0.f : (p.cache.v_scale ? __ldg(p.cache.v_scale + x.h) : 1.f) / li;
   if (nothing) z = make_float4(0.f, 0.f, 0.f, 0.f);
   uint2 two;
   two.x = half2_bits(z.x * f, z.y * f);
   two.y = half2_bits(z.z * f, z.w * f);
-  *reinterpret_cast<uint2*>(out_row(p, x, r) + d) = two;
+  *reinterpret_cast<uint2*>(p.out + ((long long)(x.first + token) * p.q_heads + head) * p.cache.head_dim + d) = two;
 }
 
 // What was left out of the products of a segment, for element d of row r: the values that are not finite among the keys that some rows
@@ -257,7 +282,7 @@ __device__ __forceinline__ void write_four(const AttentionParams& p, const Segme
 template <bool F8>
 __device__ __forceinline__ float not_finite_sum(const AttentionParams& p, const Segment& x, const Visible& sees, int tile_keys, int r, int d) {
   const KvCacheView& c = p.cache;
-  const int high = x.base_high + (x.row0 + r) / p.group, low = p.window ? max(0, high - p.window) : 0;
+  const int high = x.base_high + token_of(p, x, r), low = p.window ? max(0, high - p.window) : 0;
   float sum = 0.f;
   if (d >= c.head_dim) return sum;
 #pragma unroll 1
@@ -309,6 +334,7 @@ __device__ __forceinline__ bool join_parts(const AttentionParams& p, const Segme
     if (*(volatile int*)arrived != count - 1) return true;
     if (tid == 0) *counter = 0;
     const bool last = groups == 1 || stride > 1;
+    constexpr int kBatch = 4;  // parts whose loads are on their way together
 #pragma unroll 1
     for (int i0 = tid; i0 < rows * (DP / 4); i0 += kAtOnce * THREADS) {
       float mi[kAtOnce], li[kAtOnce];
@@ -320,11 +346,11 @@ __device__ __forceinline__ bool join_parts(const AttentionParams& p, const Segme
         z[e] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
 #pragma unroll 1
-      for (int w0 = 0; w0 < count; w0 += kGroup) {
-        float2 sums[kAtOnce][kGroup];
-        float4 u[kAtOnce][kGroup];
+      for (int w0 = 0; w0 < count; w0 += kBatch) {
+        float2 sums[kAtOnce][kBatch];
+        float4 u[kAtOnce][kBatch];
 #pragma unroll
-        for (int t = 0; t < kGroup; ++t) {
+        for (int t = 0; t < kBatch; ++t) {
           if (w0 + t >= count) break;
           const float* part = part_of(p, x, first + (w0 + t) * stride, ROWS, DP);
 #pragma unroll
@@ -338,14 +364,14 @@ __device__ __forceinline__ bool join_parts(const AttentionParams& p, const Segme
         for (int e = 0; e < kAtOnce; ++e) {
           float top = mi[e];
 #pragma unroll
-          for (int t = 0; t < kGroup; ++t)
+          for (int t = 0; t < kBatch; ++t)
             if (w0 + t < count) top = fmaxf(top, sums[e][t].x);
           const float base = top == kNone ? 0.f : top, old = exp2_fast(mi[e] - base);
           mi[e] = top;
           li[e] *= old;
           z[e].x *= old; z[e].y *= old; z[e].z *= old; z[e].w *= old;
 #pragma unroll
-          for (int t = 0; t < kGroup; ++t) {
+          for (int t = 0; t < kBatch; ++t) {
             if (w0 + t >= count) break;
             const float f = exp2_fast(sums[e][t].x - base);
             li[e] += sums[e][t].y * f;

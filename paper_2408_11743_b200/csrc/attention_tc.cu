@@ -116,21 +116,6 @@ __device__ __forceinline__ float warp_max(float x) {
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
-// bar.sync of some warps that also tells all of them whether `mine` is set for any of their threads
-__device__ __forceinline__ bool any_of(int id, int threads, bool mine) {
-  uint32_t r;
-  asm volatile(
-      "{\n"
-      ".reg .pred p, q;\n"
-      "setp.ne.u32 p, %1, 0;\n"
-      "barrier.cta.red.or.pred q, %2, %3, p;\n"
-      "selp.u32 %0, 1, 0, q;\n"
-      "}\n"
-      : "=r"(r)
-      : "r"((uint32_t)mine), "r"(id), "r"(threads)
-      : "memory");
-  return r != 0;
-}
 template <int C>
 __device__ __forceinline__ void load_columns(uint32_t taddr, float (&x)[C]) {
   if constexpr (C == 32)
@@ -625,6 +610,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   const uint32_t tmem = sh.tmem;
   pdl_launch_dependents();
   pdl_wait_prior_grids();
+  prefetch_table(p, kThreads);
   if (warp < kSoftmaxWarps) {
     if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_inc<G::kSoftmaxRegs>();
     soften<G>(p, sh, ring, weights, tmem);
