@@ -19,7 +19,9 @@ namespace marlin_b200 {
 namespace {
 
 // DP: head_dim rounded up to 64, 128 or 256.  NT: tiles of 8 rows per warp.  TW: warps side by side over the rows.
-// F8: e4m3 cache.  A stage of kTile keys is multiplied by kParts * TW warps (a group); the groups take the stages in turn.
+// F8: e4m3 cache.  A stage of kTile keys is multiplied by kParts * TW warps (a group): stage s by group s % kGroups, always.  (A wait for
+// a parity only tells the phase before the current one: two groups must not wait for consecutive fillings of one stage, which
+// may be there before an earlier stage is.)
 template <int DP_, int NT, int TW, bool F8>
 struct Geometry {
   static constexpr int DP = DP_;
@@ -231,7 +233,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
     return true;
   };
 
-  // the next tile of this group, in the numbering of all tiles of the CTA: its stage and phase
+  // the next tile of this group, in the numbering of all tiles of the CTA (tile t has stage t % kStages), its stage and phase
   uint32_t next = group, done = 0;
   int stage = group;
   uint32_t stage_phase = 0, slot_phase = 0;
@@ -300,7 +302,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
     bool open = true;  // some row has not seen a key yet
 
 #pragma unroll 1
-    for (; next < done + nt; next += G::kGroups) {
+    while (next < done + nt) {
       wait(&sh.full[stage], stage_phase);
       const uint32_t keys = ring + stage * G::kStage, values = keys + G::kHalf;
       // S^T = K Q^T: a thread has keys g, g + 8 of 16 and rows 2 t, 2 t + 1 of 8.  (One tile of rows alone would be a chain of
@@ -441,9 +443,12 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.empty[stage]);
-      stage += G::kGroups;
-      if (stage >= G::kStages) {
-        stage -= G::kStages;
+      if (stage + G::kGroups < G::kStages) {
+        stage += G::kGroups;
+        next += G::kGroups;
+      } else {  // round the ring, to this group's first stage again
+        next += G::kStages - stage + group;
+        stage = group;
         stage_phase ^= 1;
       }
     }
