@@ -130,6 +130,20 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
 #pragma unroll 1
   for (;; ++segment) {
     const Segment x = range.next(p);
+    // the page numbers of its first tiles are asked for before anything else: the first copies wait for them
+    const Visible v = visible(p, x);
+    const int* const table = c.table + x.b * c.table_stride;
+    const int key_first = x.tile * kTile + part * 16, key_end = (x.tile + x.nt) * kTile;
+    const int low = max(v.low_min, x.tile * kTile), high = min(v.high_max, key_end);
+    // pages of this part in 32 tiles, a lane each, and in the next 32; or, where pages are smaller than a part, of the keys of
+    // one tile and of the next one.  INT_MIN where no key is asked for
+    auto page_of = [&](int i) {
+      const int key = key_first + (big_pages ? i + lane : i) * kTile + (big_pages ? 0 : lane & 15);
+      return x.nt > 0 && key < high && key + (big_pages ? 16 : 1) > low ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
+    };
+    const int batch = big_pages ? 32 : 1;
+    const long long head_bytes = (x.h * c.s_head + my_row * c.s_token) * kElement + my_vec * 16;
+    int pages = page_of(0), pages_next = page_of(batch), in_batch = 0;
     if (!arrived_at(sh, &sh.closed[slot], slot_phase, p.status)) break;
     if (lane == 0 && producer == 0) sh.segments[slot] = x;
     if (x.nt > 0) {  // Q; rows and elements that are not there are zeros
@@ -137,7 +151,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
 #pragma unroll 1
       for (int i = producer * 32 + lane; i < G::kRows * G::kQVectors; i += 32 * G::kProducers) {
         const int r = i / G::kQVectors, vec = i % G::kQVectors;
-        const int token = (x.row0 + r) / p.group, head = x.h * p.group + (x.row0 + r) - token * p.group;
+        const int token = token_of(p, x, r), head = x.h * p.group + x.row0 + r - token * p.group;
         const bool there = r < x.rows && vec * 8 < c.head_dim;
         const uint16_t* src = p.q + (there ? (long long)(x.first + token) * p.q_stride + head * c.head_dim + vec * 8 : 0);
         copy16(q_to + place<G::kQVectors>(r, vec), src, there);
@@ -151,20 +165,6 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
     }
     if (x.nt == 0) break;
 
-    // ---- its tiles
-    const Visible v = visible(p, x);
-    const int* const table = c.table + x.b * c.table_stride;
-    const int key_first = x.tile * kTile + part * 16, key_end = (x.tile + x.nt) * kTile;
-    const int low = max(v.low_min, x.tile * kTile), high = min(v.high_max, key_end);
-    // pages of this part in 32 tiles, a lane each, and in the next 32; or, where pages are smaller than a part, of the keys of
-    // one tile and of the next one.  INT_MIN where no key is asked for
-    auto page_of = [&](int i) {
-      const int key = key_first + (big_pages ? i + lane : i) * kTile + (big_pages ? 0 : lane & 15);
-      return key < high && key + (big_pages ? 16 : 1) > low ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
-    };
-    const int batch = big_pages ? 32 : 1;
-    const long long head_bytes = (x.h * c.s_head + my_row * c.s_token) * kElement + my_vec * 16;
-    int pages = page_of(0), pages_next = page_of(batch), in_batch = 0;
 #pragma unroll 1
     for (int i = 0; i < x.nt; ++i, ++in_batch) {
       if (in_batch == batch) {

@@ -229,8 +229,7 @@ struct Range {
         }
       }
     }
-    Segment x;
-    x.nt = 0;
+    Segment x = {};
     if (more) {
       const uint32_t i0 = at - skip, i1 = i0 + LEAD + s.tiles, to = min(stripes.moved(end, i0, i1), i1);
       if (at < to) {

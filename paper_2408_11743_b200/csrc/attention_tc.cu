@@ -171,13 +171,31 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
 #pragma unroll 1
   for (;;) {
     const Segment x = range.next(p);
+    // the page numbers of its first tiles are asked for before anything else: the first copies wait for them
+    const Visible v = visible(p, x);
+    const int* const table = c.table + x.b * c.table_stride;
+    const int key_first = x.tile * kTile + upper * 64;
+    const int low = max(v.low_min, x.tile * kTile), high = min(v.high_max, (x.tile + x.nt) * kTile);
+    // where the four sixteens of this warp in eight tiles begin in the cache, a lane each, and in the next eight: the page number
+    // that was asked for, and what it comes to; -1 where it is not there
+    auto key_of = [&](int i) { return key_first + (i + lane / 4) * kTile + lane % 4 * 16; };
+    auto page_of = [&](int i) {
+      const int key = key_of(i);
+      return big_pages && x.nt > 0 && key < high && key + 16 > low ? __ldg(table + (key >> c.page_shift)) : -1;
+    };
+    auto place_of = [&](int i, int page) {
+      return (unsigned)page < (unsigned)c.pages
+                 ? (page * c.s_page + x.h * c.s_head + (key_of(i) & ((1 << c.page_shift) - 1)) * c.s_token) * 2 : -1ll;
+    };
+    const int page_first = page_of(0);
+    int page_next = page_of(8);
     if (!arrived_at(sh, &sh.closed[open], open_phase, p.status)) break;
     if (lane == 0 && producer == 0) sh.segments[open] = x;
     if (x.nt > 0) {  // Q; rows and elements that are not there are zeros
 #pragma unroll 1
       for (int i = producer * 32 + lane; i < G::N * kVectors; i += 32 * kProducers) {
         const int r = i / kVectors, vec = i % kVectors;
-        const int token = (x.row0 + r) / p.group, head = x.h * p.group + (x.row0 + r) - token * p.group;
+        const int token = token_of(p, x, r), head = x.h * p.group + x.row0 + r - token * p.group;
         const bool there = r < x.rows && vec * 8 < c.head_dim;
         const uint16_t* src = p.q + (there ? (long long)(x.first + token) * p.q_stride + head * c.head_dim + vec * 8 : 0);
         copy16(q_slots + open * G::kQBytes + vec / 8 * G::kQBlock + r * 128 + ((vec ^ r) & 7) * 16, src, there);
@@ -191,37 +209,28 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
     }
     if (x.nt == 0) break;
 
-    const Visible v = visible(p, x);
-    const int* const table = c.table + x.b * c.table_stride;
-    const int key_first = x.tile * kTile + upper * 64;
-    const int low = max(v.low_min, x.tile * kTile), high = min(v.high_max, (x.tile + x.nt) * kTile);
-    // pages of the four sixteens of this warp in eight tiles, a lane each, and in the next eight; INT_MIN where no key is asked for
-    auto page_of = [&](int i) {
-      const int key = key_first + (i + lane / 4) * kTile + lane % 4 * 16;
-      return big_pages && key < high && key + 16 > low ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
-    };
-    const long long head_bytes = (x.h * c.s_head + my_row * c.s_token) * 2 + my_vec * 16;
-    int pages = page_of(0), pages_next = page_of(8), in_batch = 0;
+    const long long my_bytes = my_row * c.s_token * 2 + my_vec * 16;
+    long long places = place_of(0, page_first);
+    int in_batch = 0;
     bool go_on = true;
 #pragma unroll 1
     for (int i = 0; i < x.nt; ++i, ++in_batch) {
       if (in_batch == 8) {
         in_batch = 0;
-        pages = pages_next;
-        pages_next = page_of(i + 8);
+        places = place_of(i, page_next);
+        page_next = page_of(i + 8);
       }
       const int key0 = key_first + i * kTile;
-      const bool there4 = lane / 4 != in_batch || (unsigned)pages < (unsigned)c.pages;
+      const bool there4 = lane / 4 != in_batch || places >= 0;
       const bool whole = big_pages && key0 >= low && key0 + 64 <= high && __all_sync(~0u, there4);
       go_on = arrived_at(sh, &sh.empty[slot], slot_phase, p.status);
       if (!go_on) break;
       const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (upper * 64 + my_row) * 128;
       if (whole) {
-#pragma unroll 2
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int page = __shfl_sync(~0u, pages, in_batch * 4 + j);
-          const uint8_t* src = cache;
-          if (my_part) src += (page * c.s_page + ((key0 + j * 16) & ((1 << c.page_shift) - 1)) * c.s_token) * 2 + head_bytes;
+          const long long place = __shfl_sync(~0u, places, in_batch * 4 + j);
+          const uint8_t* src = cache + (my_part ? place + my_bytes : 0);
 #pragma unroll
           for (int r = 0; r < 16; r += kPer) {
             copy16(to + (j * 16 + r) * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
