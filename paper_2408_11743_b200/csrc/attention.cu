@@ -28,16 +28,13 @@ struct Geometry {
   static constexpr int kRows = 8 * NT * TW;
   static constexpr int kTile = DP == 256 ? 32 : 64;
   static constexpr int kParts = kTile / 16;
-  // warps that multiply: as many as their registers leave room for (DP * NT / 4 sums a thread)
-  static constexpr int kConsumers = DP * NT > 128 ? 8 : F8 ? 12 : 8;
+  static constexpr int kConsumers = 8;               // warps that multiply (DP * NT / 4 sums a thread; twelve for 8 bits gained nothing)
   static constexpr int kGroups = kConsumers / (kParts * TW);
   static constexpr int kTeams = kConsumers / TW;     // warps that have the same rows
   static constexpr int kProducers = 4;
   static constexpr int kThreads = (kConsumers + kProducers) * 32;
   // The warps that copy hand registers to those that multiply, where these need more than the launch gives.
-  static constexpr int kLaunchRegs = kConsumers == 12 ? 128 : 168;
-  static constexpr int kProducerRegs = kConsumers == 12 ? 128 : 88;
-  static constexpr int kConsumerRegs = kConsumers == 12 ? 128 : 208;
+  static constexpr int kLaunchRegs = 168, kProducerRegs = 88, kConsumerRegs = 208;
   static_assert(kConsumers * kConsumerRegs + 4 * kProducerRegs <= (kConsumers + 4) * kLaunchRegs, "registers");
   static constexpr int kRowBytes = DP * (F8 ? 1 : 2);
   static constexpr int kVectors = kRowBytes / 16;    // 16-byte vectors of a key
@@ -528,7 +525,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
         }
       }
     }
-    if (!whole) join_parts<G::kRows, DP, kMine, 1>(p, x, tid, &sh.arrived, sh.ml, meet, write_out);
+    if (!whole) join_parts<G::kRows, DP, kMine, 1, 4>(p, x, tid, &sh.arrived, sh.ml, meet, write_out);
     __syncwarp();
     if (lane == 0) mbar_arrive(&sh.closed[slot]);
     if (++slot == G::kOpen) {
@@ -562,10 +559,10 @@ __global__ void __launch_bounds__(Geometry<DP, NT, TW, F8>::kThreads, 1) attenti
   pdl_wait_prior_grids();
   prefetch_table(p, G::kThreads);
   if (threadIdx.x >= G::kConsumers * 32) {
-    if constexpr (G::kProducerRegs < G::kLaunchRegs) setmaxnreg_dec<G::kProducerRegs>();
+    setmaxnreg_dec<G::kProducerRegs>();
     produce<G, F8>(p, sh, (int)threadIdx.x / 32 - G::kConsumers, smem_u32(smem), ring);
   } else {
-    if constexpr (G::kConsumerRegs > G::kLaunchRegs) setmaxnreg_inc<G::kConsumerRegs>();
+    setmaxnreg_inc<G::kConsumerRegs>();
     consume<G, NT, TW, F8>(p, sh, smem_u32(smem), reinterpret_cast<float*>(join), ring);
   }
 }
@@ -575,7 +572,7 @@ cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) 
   using G = Geometry<DP, NT, TW, F8>;
   // the warps share out the registers of the launch: with fewer of them the increase would wait for ever
   return launch_ranges<attention_kernel<DP, NT, TW, F8>, G::kSmem, G::kThreads, G::kRows, G::kTile>(
-      p, sm_count, stream, G::kConsumerRegs > G::kLaunchRegs ? G::kLaunchRegs : 0);
+      p, sm_count, stream, G::kLaunchRegs);
 }
 template <int DP, bool F8>
 cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {

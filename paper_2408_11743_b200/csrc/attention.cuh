@@ -190,7 +190,7 @@ struct Range {
     more = more && blockIdx.x < stripes.workers;
     stripes.size = stripes.total / stripes.workers;
     stripes.more = stripes.total % stripes.workers;
-    stripes.snap = stripes.size < 8 ? 2 : 0;
+    stripes.snap = stripes.size < 8 ? 2 : stripes.size < 48 ? 1 : 0;
     stripes.lead = LEAD;
     at = stripes.begin(blockIdx.x);
     end = stripes.begin(blockIdx.x + 1);
@@ -313,9 +313,9 @@ __device__ __forceinline__ float* part_of(const AttentionParams& p, const Segmen
 }
 
 // The last CTA of a group of parts joins the group, the last group the item, in the order of the keys.  For the THREADS threads
-// (tid 0 .. THREADS - 1) that `meet` brings together; ml: room for ROWS pairs; kAtOnce: vectors of a
-// thread whose loads are on their way together.  false: a wait ran out.
-template <int ROWS, int DP, int THREADS, int kAtOnce, class Meet, class WriteOut>
+// (tid 0 .. THREADS - 1) that `meet` brings together; ml: room for ROWS pairs; kAtOnce, kBatch: vectors
+// of a thread, and parts, whose loads are on their way together.  false: a wait ran out.
+template <int ROWS, int DP, int THREADS, int kAtOnce, int kBatch, class Meet, class WriteOut>
 __device__ __forceinline__ bool join_parts(const AttentionParams& p, const Segment& x, int tid, int* arrived, float2* ml, Meet meet,
                                            WriteOut write_out) {
   constexpr int kLine = part_line(DP);
@@ -333,7 +333,6 @@ __device__ __forceinline__ bool join_parts(const AttentionParams& p, const Segme
     if (*(volatile int*)arrived != count - 1) return true;
     if (tid == 0) *counter = 0;
     const bool last = groups == 1 || stride > 1;
-    constexpr int kBatch = 4;  // parts whose loads are on their way together
 #pragma unroll 1
     for (int i0 = tid; i0 < rows * (DP / 4); i0 += kAtOnce * THREADS) {
       float mi[kAtOnce], li[kAtOnce];

@@ -568,7 +568,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     }
     tc_fence_before_sync();
     auto write_out = [&](int r, int d, float4 z, float li) { write_four(p, x, r, d, z, li); };
-    if (!whole) join_parts<N, DP, kSoftmaxThreads, 2>(p, x, tid, &sh.arrived, sh.ml, meet, write_out);
+    if (!whole) join_parts<N, DP, kSoftmaxThreads, 4, 2>(p, x, tid, &sh.arrived, sh.ml, meet, write_out);
     meet();  // (bases and notes are free again)
     if (lane == 0) mbar_arrive(&sh.closed[open]);
     if (++open == G::kOpen) {
