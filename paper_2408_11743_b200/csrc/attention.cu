@@ -576,17 +576,22 @@ cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) 
 }
 template <int DP, bool F8>
 cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  // A warp holds 8 NT rows of sums (DP * NT / 4 registers a thread); more rows than that share keys and values between
-  // the warps of a team.
+  // Up to eight rows: a warp has them all beside the keys.  More of them, over fp16: the tensor cores' fifth generation (16 rows of 128
+  // elements: 39.3 us there, 39.9 here; 32 rows: 43 and 47; 48 rows: 47 and 53).  More of them over 8 bits: here, where
+  // every warp converts what it multiplies (16 rows: 31 us here, 46 there; 32 rows: 45 and 49), until the products are what takes
+  // the time, with more than 32 rows of 128 elements (48 rows: 72 and 55; of 64 elements: 44 and 46).  16 sequences of 1000 to
+  // 4099 keys, eight heads of keys.  A warp holds 8 NT rows of sums (DP * NT / 4 registers a thread); more rows than that
+  // share keys and values between the warps of a team.
   const long long rows = usual_rows(p);
   if (rows <= 8) return launch<DP, 1, 1, F8>(p, sm_count, stream);
+  if (DP < 256 && (!F8 || (DP == 128 && rows > 32))) return launch_attention_tc(p, sm_count, stream);
   if constexpr (F8 || DP == 256) {
+    constexpr int kWide = DP == 64 ? 4 : 2, kShared = DP == 64 ? 1 : 2;
     if (rows <= 16) return launch<DP, 2, 1, F8>(p, sm_count, stream);
-    if (DP == 128 || rows <= 32) return launch<DP, DP == 64 ? 4 : 2, DP == 64 ? 1 : 2, F8>(p, sm_count, stream);
-    return launch<DP, DP == 64 ? 4 : 2, DP == 64 ? 2 : DP == 128 ? 2 : 4, F8>(p, sm_count, stream);
-  } else {
-    return launch_attention_tc(p, sm_count, stream);
+    if (rows <= 32) return launch<DP, kWide, kShared, F8>(p, sm_count, stream);
+    if constexpr (DP != 128) return launch<DP, kWide, 2 * kShared, F8>(p, sm_count, stream);
   }
+  return cudaErrorInvalidValue;  // (not reached)
 }
 template <int DP>
 cudaError_t launch_format(const AttentionParams& p, int sm_count, cudaStream_t stream) {

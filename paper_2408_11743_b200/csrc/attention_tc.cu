@@ -1,5 +1,4 @@
-// Attention of new tokens over an fp16 cache where a key head has more than eight rows (heads that share keys, several new
-// tokens): the same ranges, segments and parts as attention.cu, with the products on the fifth-generation tensor cores.
+// Attention of new tokens where a key head has more than eight rows (heads that share keys, several new tokens): the same ranges, segments and parts as attention.cu, with the products on the fifth-generation tensor cores.
 //
 // A tile has 128 keys.  S^T = K Q^T with the keys as the 128 rows of the product and the rows of Q as its columns, so that thread k of
 // the softmax warps has key k and all N rows of it in its lane of tensor memory; the weights go to shared memory as P, and
@@ -15,6 +14,8 @@
 // Warps: 0 - 7 softmax and results (lane quarter w % 4 of tensor memory; 0 - 3 the first half of the rows, 4 - 7 the second, each
 // half with bases of its own), 8 and 9 copy keys, 10 and 11 values (half of every tile each), 12 and 13 issue a product each: an issue
 // costs its thread some 75 cycles and a commit 125, and with one thread for all of them everybody waited for it.
+// An 8-bit cache (of 128 elements, for more than 32 rows) is converted to fp16 by the warps that copy: the products take operands of
+// one type, and fp16 is what Q and the weights have.  The conversion bounds that: some 260 cycles for 16 keys of one warp.
 // Keys and values have rings of their own: values are held until the weights of their keys are there, and keys need not wait for that.  Tensor memory: S twice, and O; N columns each.
 #include "attention.cuh"
 #include "tc_utils.cuh"
@@ -32,10 +33,11 @@ constexpr int kIssuers = 2;
 constexpr int kThreads = 512;  // (two warps do nothing: registers are shared out by groups of four)
 static_assert(kSoftmaxThreads + (kProducers + kIssuers) * 32 <= kThreads, "warps");
 
-// DP: head_dim rounded up to 64 or 128; N: rows of a block, 16, 32 or 64
-template <int DP_, int N_>
+// DP: head_dim rounded up to 64 or 128; N: rows of a block, 16, 32 or 64; F8: e4m3 cache
+template <int DP_, int N_, bool F8_>
 struct TcGeometry {
   static constexpr int DP = DP_, N = N_;
+  static constexpr bool F8 = F8_;
   static constexpr int kHalves = DP / 64;
   static constexpr int kSlot = kHalves * kBlock;   // the keys (or the values) of a tile
   static constexpr int kQBlock = N * 128;          // 64 elements of the rows
@@ -43,16 +45,21 @@ struct TcGeometry {
   static constexpr int kOpen = 2;                  // segments that can be open at a time
   static constexpr int kPRow = 2 * N;              // weights: bytes of a key, swizzled over as many
   static constexpr int kPBytes = kTile * kPRow;
-  static constexpr int kPBuffers = 2;
+  static constexpr int kPBuffers = F8 ? 1 : 2;     // (room for the ring of the 8-bit keys)
   static constexpr bool kSumRows = DP == 64;       // the weights are summed in the product
   static constexpr int kOnes = kSumRows ? 2048 : 0;  // 16 rows of 64 ones, beside the values of 16 keys
   static constexpr int kRest = kOpen * kQBytes + kPBuffers * kPBytes + kOnes;
-  static constexpr int kSlots = (222 * 1024 - kRest) / kSlot > 12 ? 12 : (222 * 1024 - kRest) / kSlot;
+  static constexpr int kFit = (222 * 1024 - kRest) / kSlot;
+  static constexpr int kSlots = F8 ? 4 : kFit > 12 ? 12 : kFit;
+  // 8-bit caches: sixteen keys (or values) as they come, and how many of them each warp that copies has on their way
+  static constexpr int kRawBytes = 16 * DP;
+  static constexpr int kRawFit = (222 * 1024 - kRest - kSlots * kSlot) / (kProducers * kRawBytes);
+  static constexpr int kRaw = F8 ? (kRawFit > 16 ? 16 : kRawFit) : 0;
   static constexpr int kKeySlots = kSlots / 2, kValueSlots = kSlots - kKeySlots;
   // registers a thread where the launch's 128 are too few for the softmax warps (64 rows)
   static constexpr int kSoftmaxRegs = N == 64 ? 160 : 0, kOtherRegs = 96;
   static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "registers");
-  static constexpr int kSmem = kSlots * kSlot + kRest + 1024;  // (the ring begins at a multiple of 1024)
+  static constexpr int kSmem = kSlots * kSlot + kRest + kProducers * kRaw * kRawBytes + 1024;  // (the ring begins at a multiple of 1024)
   static constexpr int kColumns = 4 * N;           // of tensor memory: S, S, O, and N that a power of two brings along
   static constexpr int kMine = N / 2;              // rows of a half of the softmax warps
   static_assert(kKeySlots >= 2 && kColumns <= 512, "ring");
@@ -109,6 +116,9 @@ __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+__device__ __forceinline__ void sts128(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 // what this thread (or another whose arrival it has seen) wrote to shared memory can be read by the tensor cores
 __device__ __forceinline__ void fence_to_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float warp_max(float x) {
@@ -152,7 +162,8 @@ __device__ __forceinline__ bool arrived_at(TcShared<G>& sh, uint64_t* bar, uint3
 // ---- the warps that copy ---------------------------------------------------------------------------
 // `values`: these, not keys; `upper`: the second half of every tile
 template <class G>
-__device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& sh, bool values, bool upper, uint32_t ring, uint32_t q_slots) {
+__device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& sh, bool values, bool upper, uint32_t ring, uint32_t q_slots,
+                                        uint32_t raw) {
   const KvCacheView& c = p.cache;
   const int lane = threadIdx.x & 31, producer = 2 * values + upper;
   Range<G::N, kTile, kLead> range;
@@ -162,6 +173,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
   constexpr int kPer = 32 / kVectors;
   const int my_row = lane / kVectors, my_vec = lane % kVectors;
   const bool my_part = my_vec * 8 < c.head_dim;
+  constexpr int kElement = G::F8 ? 1 : 2;
   const bool big_pages = c.page_shift >= 4;  // sixteen keys lie in one page
   const uint8_t* const cache = static_cast<const uint8_t*>(values ? c.v : c.k);
   const long long pass = my_part ? kPer * c.s_token * 2 : 0;
@@ -185,7 +197,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
     };
     auto place_of = [&](int i, int page) {
       return (unsigned)page < (unsigned)c.pages
-                 ? (page * c.s_page + x.h * c.s_head + (key_of(i) & ((1 << c.page_shift) - 1)) * c.s_token) * 2 : -1ll;
+                 ? (page * c.s_page + x.h * c.s_head + (key_of(i) & ((1 << c.page_shift) - 1)) * c.s_token) * kElement : -1ll;
     };
     const int page_first = page_of(0);
     int page_next = page_of(8);
@@ -213,46 +225,115 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
     long long places = place_of(0, page_first);
     int in_batch = 0;
     bool go_on = true;
+    if constexpr (G::F8) {
+      // eight bits: sixteen keys at a time go to a ring of this warp as they are, where every lane later finds what it copied itself
+      constexpr int kVectors8 = G::DP / 16, kPer8 = 32 / kVectors8, kPasses = 16 / kPer8;
+      const int row8 = lane / kVectors8, vec8 = lane % kVectors8;
+      const bool part8 = vec8 * 16 < c.head_dim;
+      const long long bytes8 = row8 * c.s_token + vec8 * 16, pass8 = part8 ? kPer8 * c.s_token : 0;
+      const uint32_t mine = raw + producer * (G::kRaw * G::kRawBytes) + lane * 16;
+      const int n = 4 * x.nt;
+      auto ask = [&](int q, uint32_t to) {  // (in_batch: its tile; a group of copies even where nothing is left to ask for)
+        if (q < n) {
+          const int key0 = key_first + (q >> 2) * kTile + (q & 3) * 16;
+          const long long place = __shfl_sync(~0u, places, in_batch * 4 + (q & 3));
+          if (place >= 0 && key0 >= low && key0 + 16 <= high) {
+            const uint8_t* src = cache + (part8 ? place + bytes8 : 0);
+#pragma unroll
+            for (int j = 0; j < kPasses; ++j, src += pass8) copy16(to + j * 512, src, part8);
+          } else {
 #pragma unroll 1
-    for (int i = 0; i < x.nt; ++i, ++in_batch) {
-      if (in_batch == 8) {
-        in_batch = 0;
-        places = place_of(i, page_next);
-        page_next = page_of(i + 8);
-      }
-      const int key0 = key_first + i * kTile;
-      const bool there4 = lane / 4 != in_batch || places >= 0;
-      const bool whole = big_pages && key0 >= low && key0 + 64 <= high && __all_sync(~0u, there4);
-      go_on = arrived_at(sh, &sh.empty[slot], slot_phase, p.status);
-      if (!go_on) break;
-      const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (upper * 64 + my_row) * 128;
-      if (whole) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const long long place = __shfl_sync(~0u, places, in_batch * 4 + j);
-          const uint8_t* src = cache + (my_part ? place + my_bytes : 0);
-#pragma unroll
-          for (int r = 0; r < 16; r += kPer) {
-            copy16(to + (j * 16 + r) * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
-            src += pass;
+            for (int j = 0; j < kPasses; ++j) {
+              const int key = key0 + j * kPer8 + row8;
+              const bool asked = key >= low && key < high;
+              const long long at = asked ? cache_offset(c, __ldg(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
+              copy16(to + j * 512, cache + (at >= 0 && part8 ? at + vec8 * 16 : 0), at >= 0 && part8);
+            }
+          }
+          if ((q & 3) == 3 && ++in_batch == 8) {
+            in_batch = 0;
+            places = place_of((q >> 2) + 1, page_next);
+            page_next = page_of((q >> 2) + 9);
           }
         }
-      } else {  // pages smaller than that, the ends of a sequence, pages that are not there
-#pragma unroll 4
-        for (int r = 0; r < 64; r += kPer) {
-          const int row = r + my_row, key = key0 + row;
-          const bool asked = key >= low && key < high;
-          const long long at = asked ? cache_offset(c, __ldg(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
-          const bool there = at >= 0 && my_part;
-          copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
+        copies_commit();
+      };
+#pragma unroll 1
+      for (int q = 0; q < G::kRaw; ++q) ask(q, mine + q * G::kRawBytes);
+      uint32_t from = mine;
+#pragma unroll 1
+      for (int q = 0; q < n; ++q) {
+        if ((q & 3) == 0) {
+          go_on = arrived_at(sh, &sh.empty[slot], slot_phase, p.status);
+          if (!go_on) break;
+        }
+        copies_wait<G::kRaw - 1>();
+        const int row0 = upper * 64 + (q & 3) * 16 + row8;
+        const uint32_t to = ring + slot * G::kSlot + vec8 / 4 * kBlock + row0 * 128;
+        uint4 w[kPasses];
+#pragma unroll
+        for (int j = 0; j < kPasses; ++j) w[j] = lds128(from + j * 512);
+#pragma unroll
+        for (int j = 0; j < kPasses; ++j) {
+          const uint32_t row = to + j * kPer8 * 128, at = vec8 * 2 ^ (row0 + j * kPer8);
+          sts128(row + (at & 7) * 16, e4m3x2_to_f16x2(w[j].x), e4m3x2_to_f16x2(w[j].x >> 16), e4m3x2_to_f16x2(w[j].y), e4m3x2_to_f16x2(w[j].y >> 16));
+          sts128(row + ((at ^ 1) & 7) * 16, e4m3x2_to_f16x2(w[j].z), e4m3x2_to_f16x2(w[j].z >> 16), e4m3x2_to_f16x2(w[j].w), e4m3x2_to_f16x2(w[j].w >> 16));
+        }
+        ask(q + G::kRaw, from);
+        from = from == mine + (G::kRaw - 1) * G::kRawBytes ? mine : from + G::kRawBytes;
+        if ((q & 3) == 3) {
+          fence_to_tensor_cores();
+          mbar_arrive(&sh.full[slot]);
+          if (slot == last_slot) {
+            slot = first_slot;
+            slot_phase ^= 1;
+          } else {
+            ++slot;
+          }
         }
       }
-      copies_arrive(&sh.full[slot]);
-      if (slot == last_slot) {
-        slot = first_slot;
-        slot_phase ^= 1;
-      } else {
-        ++slot;
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < x.nt; ++i, ++in_batch) {
+        if (in_batch == 8) {
+          in_batch = 0;
+          places = place_of(i, page_next);
+          page_next = page_of(i + 8);
+        }
+        const int key0 = key_first + i * kTile;
+        const bool there4 = lane / 4 != in_batch || places >= 0;
+        const bool whole = big_pages && key0 >= low && key0 + 64 <= high && __all_sync(~0u, there4);
+        go_on = arrived_at(sh, &sh.empty[slot], slot_phase, p.status);
+        if (!go_on) break;
+        const uint32_t to = ring + slot * G::kSlot + my_vec / 8 * kBlock + (upper * 64 + my_row) * 128;
+        if (whole) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const long long place = __shfl_sync(~0u, places, in_batch * 4 + j);
+            const uint8_t* src = cache + (my_part ? place + my_bytes : 0);
+#pragma unroll
+            for (int r = 0; r < 16; r += kPer) {
+              copy16(to + (j * 16 + r) * 128 + ((my_vec ^ (r + my_row)) & 7) * 16, src, my_part);
+              src += pass;
+            }
+          }
+        } else {  // pages smaller than that, the ends of a sequence, pages that are not there
+#pragma unroll 4
+          for (int r = 0; r < 64; r += kPer) {
+            const int row = r + my_row, key = key0 + row;
+            const bool asked = key >= low && key < high;
+            const long long at = asked ? cache_offset(c, __ldg(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
+            const bool there = at >= 0 && my_part;
+            copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
+          }
+        }
+        copies_arrive(&sh.full[slot]);
+        if (slot == last_slot) {
+          slot = first_slot;
+          slot_phase ^= 1;
+        } else {
+          ++slot;
+        }
       }
     }
     if (!go_on) break;
@@ -360,7 +441,8 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       meet_half();
     }
     bool fresh = true;  // some row has not seen a key yet
-    const float hidden = p.scale_log2 < 0.f ? INFINITY : -INFINITY;
+    const float factor = p.scale_log2 * (G::F8 && c.k_scale ? __ldg(c.k_scale + x.h) : 1.f);
+    const float hidden = factor < 0.f ? INFINITY : -INFINITY;
     float l[kMine];     // (kSumRows: not used)
 #pragma unroll
     for (int r = 0; r < kMine; ++r) l[r] = 0.f;
@@ -391,7 +473,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         for (int r = 0; r < kMine; r += 4) {
           // (row r + warp % 4, without an index that is not known to the compiler)
           const float z = (warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]);
-          const float top = warp_max(z == hidden ? kNone : z * p.scale_log2);
+          const float top = warp_max(z == hidden ? kNone : z * factor);
           none |= top == kNone;
           if (lane == 0) {
             sh.largest[mine + r + (warp & 3)] = top;
@@ -405,10 +487,10 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
 #pragma unroll
       for (int r = 0; r < kMine; r += 4) {
         const float4 base = *reinterpret_cast<const float4*>(&sh.base[mine + r]);
-        y[r] = fmaf(y[r], p.scale_log2, -base.x);
-        y[r + 1] = fmaf(y[r + 1], p.scale_log2, -base.y);
-        y[r + 2] = fmaf(y[r + 2], p.scale_log2, -base.z);
-        y[r + 3] = fmaf(y[r + 3], p.scale_log2, -base.w);
+        y[r] = fmaf(y[r], factor, -base.x);
+        y[r + 1] = fmaf(y[r + 1], factor, -base.y);
+        y[r + 2] = fmaf(y[r + 2], factor, -base.z);
+        y[r + 3] = fmaf(y[r + 3], factor, -base.w);
         top = fmaxf(fmaxf(fmaxf(top, y[r]), fmaxf(y[r + 1], y[r + 2])), y[r + 3]);
       }
       const bool over = fresh || top > kSlack;
@@ -530,10 +612,11 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     uint16_t* to_out = p.out + ((long long)(x.first + token) * p.q_heads + x.h * p.group + head) * c.head_dim + key;
     float* to_part = part_of(p, x, blockIdx.x, N, DP) + mine * kLine;
     const int next_token = (p.q_heads - p.group) * c.head_dim;
+    const float values_of = G::F8 && c.v_scale ? __ldg(c.v_scale + x.h) : 1.f;
     auto give = [&](int r, float z) {
       const float sum = sh.alpha[r];
       if (whole) {
-        const __half y = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z, sum));
+        const __half y = __float2half_rn(x.base_high + token <= 0 ? 0.f : __fdividef(z * values_of, sum));
         if (key < c.head_dim) *to_out = *reinterpret_cast<const uint16_t*>(&y);
         to_out += c.head_dim;
         if (++head == p.group) {
@@ -553,7 +636,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         float z;
         load_column(lanes + 2 * N + r, z);
         tc_wait_ld();
-        give(r, z + not_finite_sum<false>(p, x, sees, kTile, r, key));
+        give(r, z + not_finite_sum<G::F8>(p, x, sees, kTile, r, key));
       }
     } else {
 #pragma unroll 1
@@ -578,9 +661,9 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
   }
 }
 
-template <int DP, int N>
+template <int DP, int N, bool F8>
 __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const AttentionParams p) {
-  using G = TcGeometry<DP, N>;
+  using G = TcGeometry<DP, N, F8>;
   extern __shared__ uint8_t smem[];
   __shared__ TcShared<G> sh;
   const uint32_t ring = (smem_u32(smem) + 1023u) & ~1023u;
@@ -627,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
     if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_dec<G::kOtherRegs>();
     const int w = warp - kSoftmaxWarps;
     if (w < kProducers)
-      produce<G>(p, sh, w / 2, w % 2, ring, q_slots);
+      produce<G>(p, sh, w / 2, w % 2, ring, q_slots, ones + G::kOnes);
     else if (w == kProducers && threadIdx.x % 32 == 0)
       multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
     else if (w == kProducers + 1 && threadIdx.x % 32 == 0)
@@ -642,22 +725,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   }
 }
 
-template <int DP, int N>
+template <int DP, int N, bool F8>
 cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) {
-  using G = TcGeometry<DP, N>;
-  return launch_ranges<attention_tc_kernel<DP, N>, G::kSmem, kThreads, N, kTile>(p, sm_count, stream, G::kSoftmaxRegs ? 128 : 0);
+  using G = TcGeometry<DP, N, F8>;
+  return launch_ranges<attention_tc_kernel<DP, N, F8>, G::kSmem, kThreads, N, kTile>(p, sm_count, stream, G::kSoftmaxRegs ? 128 : 0);
 }
 template <int DP>
 cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
   const long long rows = usual_rows(p);
-  if (rows <= 16) return launch<DP, 16>(p, sm_count, stream);
-  if (rows <= 32) return launch<DP, 32>(p, sm_count, stream);
-  return launch<DP, 64>(p, sm_count, stream);
+  if (rows <= 16) return launch<DP, 16, false>(p, sm_count, stream);
+  if (rows <= 32) return launch<DP, 32, false>(p, sm_count, stream);
+  return launch<DP, 64, false>(p, sm_count, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_attention_tc(const AttentionParams& p, int sm_count, cudaStream_t stream) {
+  if (p.cache.eight_bit) return launch<128, 64, true>(p, sm_count, stream);
   return padded_dim(p.cache.head_dim) == 64 ? launch_rows<64>(p, sm_count, stream) : launch_rows<128>(p, sm_count, stream);
 }
 

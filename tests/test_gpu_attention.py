@@ -40,7 +40,8 @@ EDGES = [0, 1, 2, 15, 16, 17, 48, 63, 64, 65, 100, 127, 128, 129, 700]
 
 @pytest.mark.parametrize("q_heads,kv_heads,dim,page", [
     (4, 4, 128, 16), (8, 1, 128, 16), (16, 2, 64, 32), (29, 1, 64, 8), (71, 1, 64, 16), (3, 3, 80, 16), (4, 2, 16, 4), (6, 2, 48, 64),
-    (8, 2, 256, 16), (40, 1, 256, 32), (2, 2, 192, 1), (5, 1, 112, 256), (64, 2, 128, 2), (17, 1, 128, 128), (130, 2, 32, 16)])
+    (8, 2, 256, 16), (40, 1, 256, 32), (2, 2, 192, 1), (5, 1, 112, 256), (64, 2, 128, 2), (17, 1, 128, 128), (130, 2, 32, 16),
+    (40, 1, 128, 16), (96, 2, 112, 8), (34, 1, 128, 1)])
 @pytest.mark.parametrize("eight_bit", [False, True])
 def test_single_tokens_at_every_edge_of_the_lengths(marlin, q_heads, kv_heads, dim, page, eight_bit):
     case = Case(EDGES, 1, q_heads, kv_heads, dim, page, eight_bit, seed=q_heads + dim)
@@ -51,7 +52,8 @@ def test_single_tokens_at_every_edge_of_the_lengths(marlin, q_heads, kv_heads, d
 
 @pytest.mark.parametrize("q_heads,kv_heads,dim,new", [
     (8, 8, 128, [3, 0, 5, 1, 2, 4, 6, 0]), (16, 2, 128, [6, 1, 2, 6, 0, 3, 4, 5]), (32, 1, 64, [1, 2, 3, 4, 5, 4, 3, 2]),
-    (4, 1, 256, [9, 16, 1, 0, 4, 17, 2, 3]), (7, 1, 80, [40, 1, 70, 3, 5, 64, 2, 1])])
+    (4, 1, 256, [9, 16, 1, 0, 4, 17, 2, 3]), (7, 1, 80, [40, 1, 70, 3, 5, 64, 2, 1]),
+    (24, 2, 128, [9, 1, 3, 5, 6, 4, 2, 8])])
 @pytest.mark.parametrize("eight_bit", [False, True])
 @pytest.mark.parametrize("window", [0, 1, 37, 64, 150])
 def test_several_new_tokens_and_windows(marlin, q_heads, kv_heads, dim, new, eight_bit, window):
@@ -76,13 +78,13 @@ def test_layouts_of_the_cache(marlin, layout, eight_bit):
     check(case, run(marlin, case))
 
 
-@pytest.mark.parametrize("lengths,q_heads,kv_heads,new", [
-    ([33001], 8, 8, 1), ([20000, 3, 9000], 8, 1, 1), ([16384, 16385], 24, 1, [3, 4]), ([50] * 700, 2, 2, 1),
-    (list(range(1, 300)), 4, 1, 1)])
+@pytest.mark.parametrize("lengths,q_heads,kv_heads,new,dim", [
+    ([33001], 8, 8, 1, 64), ([20000, 3, 9000], 8, 1, 1, 64), ([16384, 16385], 24, 1, [3, 4], 64), ([50] * 700, 2, 2, 1, 64),
+    (list(range(1, 300)), 4, 1, 1, 64), ([9000, 40, 12345], 16, 1, [3, 4, 3], 128), ([70] * 300, 40, 1, 1, 128)])
 @pytest.mark.parametrize("eight_bit", [False, True])
-def test_long_sequences_and_many(marlin, lengths, q_heads, kv_heads, new, eight_bit):
+def test_long_sequences_and_many(marlin, lengths, q_heads, kv_heads, new, dim, eight_bit):
     # parts of one sequence on many CTAs, several sequences on one CTA
-    case = Case(lengths, new, q_heads, kv_heads, 64, 16, eight_bit, seed=len(lengths))
+    case = Case(lengths, new, q_heads, kv_heads, dim, 16, eight_bit, seed=len(lengths))
     d = case.dev(marlin)
     d["workspace"][8192:] = 0xFF  # slots are written before they are read
     first = run(marlin, case, d=d)
@@ -126,10 +128,10 @@ def test_values_that_no_token_sees_do_not_matter(marlin):
 
 
 @pytest.mark.parametrize("eight_bit", [False, True])
-@pytest.mark.parametrize("q_heads", [2, 12, 24])
-def test_infinities_and_nan_reach_the_tokens_that_see_them_alone(marlin, q_heads, eight_bit):
+@pytest.mark.parametrize("q_heads,dim", [(2, 64), (12, 64), (24, 64), (3, 128), (12, 128)])
+def test_infinities_and_nan_reach_the_tokens_that_see_them_alone(marlin, q_heads, dim, eight_bit):
     import torch
-    case = Case([40, 80], [5, 4], q_heads, 1, 64, 16, eight_bit, seed=9)
+    case = Case([40, 80], [5, 4], q_heads, 1, dim, 16, eight_bit, seed=9)
     d = case.dev(marlin)
     want = run(marlin, case, d=d)
     k, v = d["k_cache"].clone(), d["v_cache"].clone()
@@ -143,8 +145,8 @@ def test_infinities_and_nan_reach_the_tokens_that_see_them_alone(marlin, q_heads
     else:
         v[at(0, 38)][7], v[at(0, 37)][8], v[at(0, 38)][9], v[at(0, 37)][10], v[at(0, 39)][10] = nan, inf, -inf, inf, -inf
         k[at(1, 79)][:] = nan
-    got = run(marlin, case, d={**d, "k_cache": k, "v_cache": v}).view(9, q_heads, 64)
-    want = want.view(9, q_heads, 64).clone()
+    got = run(marlin, case, d={**d, "k_cache": k, "v_cache": v}).view(9, q_heads, dim)
+    want = want.view(9, q_heads, dim).clone()
     # sequence 0 has positions 35 .. 39 in rows 0 .. 4, sequence 1 76 .. 79 in rows 5 .. 8
     want[3:5, :, 7] = nan
     if not eight_bit:
