@@ -109,14 +109,18 @@ def spill_report():
 
 
 TC_LAUNCH_REGS = 96  # kLaunchRegs of csrc/gemm_tc.cuh
+# kernels whose warps share out their registers, and how many a thread they are launched with: the same, Geometry::kLaunchRegs of
+# csrc/attention.cu, and all that 512 threads can have in csrc/attention_tc.cu
+LAUNCH_REGS = {"gemm_tc_kernel": TC_LAUNCH_REGS, "attention_kernel": 168, "attention_tc_kernel": 128}
 
 
 def check_registers(report):
-    """The warps of the tcgen05 kernels share out the registers that a block is launched with, so these kernels launch with
+    """The warps of some kernels share out the registers that a block is launched with, so these kernels launch with
     exactly that many or not at all: a compiler that takes another number shows here, not in every call."""
-    off = {k: v[0] for k, v in report.items() if "gemm_tc_kernel" in k and v[0] != TC_LAUNCH_REGS}
-    if off:
-        raise RuntimeError(f"tcgen05 kernels compiled to other than {TC_LAUNCH_REGS} registers a thread: {off}")
+    for kernel, regs in LAUNCH_REGS.items():
+        off = {k: v[0] for k, v in report.items() if kernel in k and v[0] != regs}
+        if off:
+            raise RuntimeError(f"{kernel} compiled to other than {regs} registers a thread: {off}")
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=(), out: str = LIB) -> str:

@@ -201,7 +201,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
           if (with_values) copy16(dst + G::kHalf, static_cast<const uint8_t*>(c.v) + bytes, there);
         }
       }
-      copies_arrive(&sh.full[stage]);
+      if (!withheld(p, producer == 0 && stage == 0)) copies_arrive(&sh.full[stage]);
       if (++stage == G::kStages) {
         stage = 0;
         stage_phase ^= 1;

@@ -34,6 +34,14 @@ template <int N>
 __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+// test builds: worker 0 leaves out an arrival that it owes (kTestWithholdMagic)
+__device__ __forceinline__ bool withheld(const AttentionParams& p, bool owed) {
+#ifdef MARLIN_TEST_HOOKS
+  return owed && blockIdx.x == 0 && p.status[7] == kTestWithholdMagic;
+#else
+  return false;
+#endif
+}
 __device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;

@@ -283,7 +283,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
         from = from == mine + (G::kRaw - 1) * G::kRawBytes ? mine : from + G::kRawBytes;
         if ((q & 3) == 3) {
           fence_to_tensor_cores();
-          mbar_arrive(&sh.full[slot]);
+          if (!withheld(p, slot == 0)) mbar_arrive(&sh.full[slot]);
           if (slot == last_slot) {
             slot = first_slot;
             slot_phase ^= 1;
@@ -327,7 +327,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
             copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
           }
         }
-        copies_arrive(&sh.full[slot]);
+        if (!withheld(p, slot == 0)) copies_arrive(&sh.full[slot]);
         if (slot == last_slot) {
           slot = first_slot;
           slot_phase ^= 1;

@@ -1,0 +1,89 @@
+"""GPU: the bounded waits of the attention kernels expire, report, and leave the device usable.
+
+As for the products (test_gpu_timeout.py): a test build of the library, with waits of a few milliseconds and a hook by which one CTA
+leaves out an arrival when a magic word sits in the workspace.  Nothing is faulted, trapped or hung.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+
+from cache_util import Case, attention_bound
+
+pytestmark = pytest.mark.gpu
+
+WITHHOLD_MAGIC = 0x57495448
+
+
+@pytest.fixture(scope="module")
+def marlin():
+    import torch
+    assert torch.cuda.is_available()
+    import paper_2408_11743_b200 as m
+    m.lib()
+    return m
+
+
+@pytest.fixture(scope="module")
+def test_lib(tmp_path_factory):
+    from paper_2408_11743_b200 import binding, build
+    out = str(tmp_path_factory.mktemp("marlin_test_build") / "libmarlin_b200_testhooks.so")
+    build.build(extra_flags=["-DMARLIN_TEST_HOOKS", "-DMARLIN_WAIT_LIMIT_NS=5000000ull"], out=out)
+    lib = ctypes.CDLL(out)
+    vp, i, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+    lib.marlin_attention_decode.argtypes = [vp, ctypes.c_int64, ctypes.POINTER(binding.KvCache), vp, i, i, ctypes.c_float, i, vp, vp, sz, vp]
+    lib.marlin_attention_decode.restype = i
+    lib.marlin_read_status.argtypes = [vp, vp]
+    lib.marlin_read_status.restype = i
+    return lib
+
+
+# every kernel: rows beside the keys, on tcgen05, and there with conversion; several tiles of one sequence for worker 0
+@pytest.mark.parametrize("q_heads,eight_bit", [(4, False), (4, True), (16, False), (40, False), (40, True)])
+def test_an_expired_wait_is_reported_and_the_next_call_is_correct(marlin, test_lib, q_heads, eight_bit):
+    import torch
+    from paper_2408_11743_b200 import binding
+    case = Case([130000, 700], 1, q_heads, 1, 128, 16, eight_bit, seed=q_heads)  # (so long that worker 0 has a part of it for certain)
+    d = case.dev(marlin)
+    q = torch.from_numpy(case.q.reshape(case.T, -1)).cuda()
+    out = torch.zeros_like(q)
+    ws = d["workspace"]
+    stream = torch.cuda.current_stream().cuda_stream
+    k, v = d["k_cache"], d["v_cache"]
+    cache = binding.KvCache(
+        k=k.data_ptr(), v=v.data_ptr(), stride=(ctypes.c_int64 * 3)(*k.stride()[:3]), table=d["pages"].data_ptr(),
+        table_stride=d["pages"].stride(0), lengths=d["lengths"].data_ptr(),
+        k_scale=d["k_scale"].data_ptr() if eight_bit else None, v_scale=d["v_scale"].data_ptr() if eight_bit else None,
+        pages=case.pages, max_pages=d["pages"].shape[1], sequences=case.B, kv_heads=1, head_dim=128, page_size=16,
+        format=int(eight_bit))
+
+    def call():
+        return test_lib.marlin_attention_decode(q.data_ptr(), q.stride(0), ctypes.byref(cache), None, case.T, q_heads, 0.125, 0,
+                                                out.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+
+    ref = case.attention_ref(0.125)
+
+    def check(got):
+        assert np.all(np.abs(got.float().cpu().numpy().reshape(ref[0].shape) - ref[0]) <= attention_bound(ref))
+
+    assert call() == 0
+    assert test_lib.marlin_read_status(ws.data_ptr(), stream) == 0
+    check(out)
+
+    ws[:32].view(torch.int32)[7] = WITHHOLD_MAGIC
+    assert call() == 0
+    torch.cuda.synchronize()  # the kernel returns through its normal control flow
+    assert test_lib.marlin_read_status(ws.data_ptr(), stream) == 8  # MARLIN_ERR_DEVICE_TIMEOUT
+    rec = ws[:32].cpu().numpy().view(np.int32)
+    assert rec[0] == 8 and rec[1] == 0
+    assert 0 <= rec[2] < 1024 and rec[5] > 0
+    assert rec[6] >= 4000  # (in units of 1.024 us)
+
+    ws.zero_()
+    out.fill_(float("nan"))
+    assert call() == 0
+    assert test_lib.marlin_read_status(ws.data_ptr(), stream) == 0
+    check(out)
+    ws2 = torch.zeros_like(ws)
+    check(marlin.attention_decode(q, k, v, d["pages"], d["lengths"], ws2, scale=0.125, k_scale=d.get("k_scale"), v_scale=d.get("v_scale")))
+    assert marlin.read_status(ws2) == 0
