@@ -285,7 +285,7 @@ typedef struct {
  * and behind starts[sequences] belong to nobody: neither the cache nor their rows of the outputs are written.  A token whose position
  * would be negative (a sequence with fewer tokens than rows, for example an empty one of a padded batch) is not put
  * into the cache; its rows of the outputs are zeros.
- * A length outside of 0 .. max_pages * page_size is taken as the nearest of the two, a page number outside of 0 .. pages - 1 as a page
+ * A length outside of 0 .. max_pages * page_size (or 2^30, if that is less) is taken as the nearest of the two, a page number outside of 0 .. pages - 1 as a page
  * that is not there (nothing is written to it, attention reads zeros for it); both set the status word to MARLIN_ERR_CACHE. */
 
 /* Bytes of workspace of the three calls below on heads of head_dim elements (0: not supported; host arithmetic only).
@@ -317,9 +317,11 @@ MARLIN_API int marlin_kv_append(const void* q, int64_t q_stride, const void* k, 
  *   out        device, out, fp16 [tokens][q_heads * head_dim]
  * out = sum_j w_j v_j, w = softmax over the positions j <= p, j > p - window of scale * q . k_j, p the token's position;
  * zeros where there is none.  Values at other positions never reach a result, whatever they are (infinities, NaN).
- * One launch: the tiles of 64 keys of all sequences and key heads are numbered through and cut into equal ranges, one
- * per CTA (the stripes of Section 3.4 "Striped Partitioning"); parts of a sequence are joined by the CTA that comes last,
- * in the order of the keys, so that the same inputs give the same bits on every call.  Sums and the softmax are fp32.
+ * One launch: the tiles of 32 to 128 keys of all sequences and key heads are numbered through and cut into about equal ranges,
+ * one per CTA (the stripes of Section 3.4 "Striped Partitioning"); parts of a sequence are joined by the CTA that comes
+ * last, in the order of the keys, so that the same inputs give the same bits on every call.  Sums and the softmax are fp32;
+ * a weight is rounded to fp16 before it is multiplied with a value.  A call of more than 2^30 tiles is refused on the
+ * device (MARLIN_ERR_CACHE, nothing is written).
  * Any number of tokens per sequence is right; it is made for one and the few of speculative decoding (bound by reading the cache). */
 MARLIN_API int marlin_attention_decode(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const int32_t* starts,
                             int tokens, int q_heads, float scale, int window, void* out,

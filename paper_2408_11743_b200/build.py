@@ -9,6 +9,7 @@ cross-compiles without a GPU.
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 
@@ -41,7 +42,6 @@ def native_path() -> str:
     """Where the extension module for this Python and this torch lies.  It is compiled against the C++ headers of the one
     and the object layouts of the other, so both are part of its name: after an upgrade the old file is not found (and
     not loaded) instead of misreading tensors."""
-    import re
     import sysconfig
     import torch
     tag = f"{sysconfig.get_config_var('SOABI')}-torch-{torch.__version__}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
@@ -84,7 +84,6 @@ PTXAS_LOG = os.path.join(_HERE, "ptxas_report.log")
 
 def spill_report():
     """{kernel name: (registers, spill store bytes)} from the last build of the product library, or {} if there is none."""
-    import re
     try:
         text = open(PTXAS_LOG).read()
     except OSError:
@@ -110,15 +109,15 @@ def spill_report():
 
 TC_LAUNCH_REGS = 96  # kLaunchRegs of csrc/gemm_tc.cuh
 # kernels whose warps share out their registers, and how many a thread they are launched with: the same, Geometry::kLaunchRegs of
-# csrc/attention.cu, and all that 512 threads can have in csrc/attention_tc.cu
-LAUNCH_REGS = {"gemm_tc_kernel": TC_LAUNCH_REGS, "attention_kernel": 168, "attention_tc_kernel": 128}
+# csrc/attention.cu, and all that 512 threads can have in csrc/attention_tc.cu (with blocks of 64 rows)
+LAUNCH_REGS = {"gemm_tc_kernel": TC_LAUNCH_REGS, "attention_kernel": 168, r"attention_tc_kernelILi\d+ELi64E": 128}
 
 
 def check_registers(report):
     """The warps of some kernels share out the registers that a block is launched with, so these kernels launch with
     exactly that many or not at all: a compiler that takes another number shows here, not in every call."""
     for kernel, regs in LAUNCH_REGS.items():
-        off = {k: v[0] for k, v in report.items() if kernel in k and v[0] != regs}
+        off = {k: v[0] for k, v in report.items() if re.search(kernel, k) and v[0] != regs}
         if off:
             raise RuntimeError(f"{kernel} compiled to other than {regs} registers a thread: {off}")
 

@@ -541,8 +541,13 @@ static int check_attention(const void* q, int64_t q_stride, const marlin_kv_cach
   p->tokens = tokens;
   p->q_heads = q_heads;
   p->group = q_heads / cache->kv_heads;
-  p->window = window;
+  // (a window that no sequence can fill is none)
+  p->window = window >= (1 << 30) || window >= (long long)cache->max_pages * cache->page_size ? 0 : window;
   p->scale_log2 = scale * 1.44269504088896340736f;
+  // lines of 128 bytes, from the first number to the last; of a table of more than 8 MB, mostly entries that no sequence has
+  // reached, the rest stays where it is
+  const long long numbers = (cache->sequences - 1) * cache->table_stride + cache->max_pages;
+  p->table_lines = (int)(numbers < (1 << 21) ? (numbers + 31) / 32 : 1 << 16);
   return MARLIN_OK;
 }
 

@@ -441,8 +441,9 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       meet_half();
     }
     bool fresh = true;  // some row has not seen a key yet
-    const float factor = p.scale_log2 * (G::F8 && c.k_scale ? __ldg(c.k_scale + x.h) : 1.f);
-    const float hidden = factor < 0.f ? INFINITY : -INFINITY;
+    const float scale = p.scale_log2 * (G::F8 && c.k_scale ? __ldg(c.k_scale + x.h) : 1.f);
+    // (a hidden logit is an infinity, and would not stay one under 0: products of finite numbers times 1e-30 have weights of 1 all the same)
+    const float factor = scale == 0.f ? 1e-30f : scale, hidden = factor < 0.f ? INFINITY : -INFINITY;
     float l[kMine];     // (kSumRows: not used)
 #pragma unroll
     for (int r = 0; r < kMine; ++r) l[r] = 0.f;

@@ -9,10 +9,12 @@ namespace marlin_b200 {
 // The first report of a call that reaches outside of the cache; a time-out that is already there stays.
 __device__ __forceinline__ void report_cache(int* status) { atomicCAS(status, 0, (int)MARLIN_ERR_CACHE); }
 
+constexpr int kLongest = 1 << 30;  // tokens of a sequence: positions, windows in front of them and tiles asked for ahead fit in 32 bits
+
 // Length of sequence b, kept inside of what its row of the table can hold.
 __device__ __forceinline__ int cache_length(const KvCacheView& c, int b, int* status) {
   const int len = __ldg(c.lengths + b);
-  const long long most = (long long)c.max_pages << c.page_shift;
+  const long long most = min((long long)c.max_pages << c.page_shift, (long long)kLongest);
   if (len < 0 || len > most) {
     report_cache(status);
     return len < 0 ? 0 : (int)most;

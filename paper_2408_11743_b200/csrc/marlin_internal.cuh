@@ -156,6 +156,7 @@ struct AttentionParams {
   int tokens, q_heads, group;  // group: query heads per key head
   int window;            // 0: none
   float scale_log2;      // scale * log2(e)
+  int table_lines;   // of the page table: asked for before anything else
 };
 size_t attention_slot_bytes(int head_dim);
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream);

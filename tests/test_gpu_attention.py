@@ -105,6 +105,28 @@ def test_scale_and_column_ranges(marlin):
         check(case, out, scale=scale)
 
 
+@pytest.mark.parametrize("q_heads", [4, 12, 20, 40])
+@pytest.mark.parametrize("eight_bit", [False, True])
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+def test_scales_that_are_not_positive(marlin, q_heads, eight_bit, scale):
+    # what is hidden stays hidden: in the last tile, around the new tokens and at the edge of a window
+    for new, window in ((1, 0), ([3, 1, 2, 5], 0), ([3, 1, 2, 5], 30)):
+        case = Case([70, 1, 130, 129], new, q_heads, 1, 128, 16, eight_bit, seed=q_heads)
+        if eight_bit and scale:  # (a sign of its own)
+            case.k_scale = -case.k_scale
+        check(case, run(marlin, case, window, scale=scale), window, scale=scale)
+
+
+@pytest.mark.parametrize("q_heads", [4, 20])
+def test_windows_as_long_as_can_be(marlin, q_heads):
+    import torch
+    case = Case([3, 40, 300], [5, 2, 1], q_heads, 1, 64, 16, seed=q_heads)
+    d = case.dev(marlin)
+    plain = run(marlin, case, d=d)
+    for window in (2 ** 31 - 1, 2 ** 30, case.table.shape[1] * 16):
+        assert torch.equal(run(marlin, case, window, d=d), plain)
+
+
 def test_values_that_no_token_sees_do_not_matter(marlin):
     # everything that is not a key or a value of some sequence is NaN, also behind the last token on its page
     import torch
