@@ -8,11 +8,18 @@
 //
 // What bounds it: the cache is read once (2 * 2 * head_dim bytes per key and key head), at 8 rows for 4 * 8 * head_dim
 // operations of the tensor cores: 8 operations a byte, so the copies have to be kept in flight and little else counts.  One CTA
-// per SM: a warp that does nothing but follow the range and issue copies (16 bytes each, addresses by key, so that a page may
-// end anywhere) into a ring of stages, and warps that multiply what has arrived, one 16-key part of a stage each.  The copies run ahead
-// over the ends of segments, so the next sequence's keys are on their way while this one's sums are joined.
+// per SM: four warps that do nothing but follow the range and issue copies (16 bytes each, addresses by key, so that a page may
+// end anywhere) into a ring of stages of all the shared memory there is, and eight warps that multiply what has arrived, one
+// 16-key part of a stage each.  (An issue of a copy takes a warp 33 cycles: with one warp that copied, it was what bounded the kernel.)
+// The copies run ahead over the ends of segments, so the next sequence's keys are on their way while this one's sums are joined.
 // The products are mma.sync.m16n8k16 with the keys (of S^T = K Q^T) and the values (of O^T = V^T P^T) on the 16-wide side and
 // the rows on the 8-wide one: a decode step has few rows, and eight of them fill an operand.
+//
+// Measured, back to back in a graph: 64 sequences of 2000 to 4096 keys, 32 heads of 128 elements, 456 us, 7.0 TB/s; 64 of up to 8191 keys that
+// eight query heads share, 160 us, 6.7 TB/s; one of 131009 keys, 88 us, 6.1 TB/s; 16 of 500 to 1531 keys, 47 us, 5.8 TB/s: a call costs some
+// 8.5 us beside the time of its bytes, of which 4 pass before the first products (launch, ranges, page numbers, first keys) and 4 in
+// CTAs that end before others and in the joining of parts; one of 129 keys takes 5.9.  8-bit caches, 32 of 2000 to 4099 keys: 44 us,
+// 4.6 TB/s, where the copies alone take 38: every element is converted by the warp that multiplies it.
 #include "attention.cuh"
 
 namespace marlin_b200 {

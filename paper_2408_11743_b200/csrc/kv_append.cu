@@ -5,6 +5,10 @@
 // cosines once, while the loads of all threads are on their way, and every 16-byte vector is read once and written once.
 // t is formed in 64 bits and reduced by whole turns there: the rounding of a 32-bit product alone would be off by 2^-24 t,
 // half a percent of a radian at position 10^5.
+//
+// What bounds it: the bytes where there are many tokens (10800 of them with 32 heads each of queries, keys and values: 97 us, 5.5 TB/s, of reads and
+// writes in equal parts), and one chain of dependent loads (length, page number, then the stores) where there are few: 2.5 us for one
+// token, 3.5 for 64.
 #include "kv_cache.cuh"
 
 namespace marlin_b200 {
