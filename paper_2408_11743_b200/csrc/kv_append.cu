@@ -6,9 +6,10 @@
 // t is formed in 64 bits and reduced by whole turns there: the rounding of a 32-bit product alone would be off by 2^-24 t,
 // half a percent of a radian at position 10^5.
 //
-// What bounds it: the bytes where there are many tokens (10800 of them with 32 heads each of queries, keys and values: 97 us, 5.5 TB/s, of reads and
-// writes in equal parts), and one chain of dependent loads (length, page number, then the stores) where there are few: 2.5 us for one
-// token, 3.5 for 64.
+// What bounds it: the bytes where there are many tokens (10800 of them with 32 heads each of queries, keys and values: 82 us, 6.5 TB/s, of
+// reads and writes in equal parts, as fast as a copy; 97 us with divisions by run-time numbers in place of multiplications and with
+// sines that lay in the order of the pairs, four lanes to a bank: 62 % of the issue slots were taken), and one chain of dependent
+// loads (length, page number, then the stores) where there are few: 2.2 us for one token, 2.8 for 64.
 #include "kv_cache.cuh"
 
 namespace marlin_b200 {
@@ -24,18 +25,22 @@ struct Unit {
   bool turned;
 };
 
+// u / d for magic = magic_of(d): (u * ceil(2^31 / d)) >> 31 is off by less than u * d / 2^31 of a step of 1 / d, and u * d < 2^28 here
+__device__ __forceinline__ int divided(int u, uint32_t magic) { return (int)__umulhi(2u * (uint32_t)u, magic); }
+uint32_t magic_of(int d) { return ((1u << 31) + (uint32_t)d - 1) / (uint32_t)d; }
+
 __device__ __forceinline__ Unit unit_of(const AppendParams& p, int u) {
   const int turning = (p.q_heads + p.cache.kv_heads) * p.head_units;
   Unit r;
   if (u >= turning) {
     const int w = u - turning, per = p.cache.head_dim / 8;
-    r.head = w / per;
+    r.head = divided(w, p.value_magic);
     r.at = (w - r.head * per) * 8;
     r.head += p.q_heads + p.cache.kv_heads;
     r.pair = r.turned = false;
     return r;
   }
-  r.head = u / p.head_units;
+  r.head = divided(u, p.head_magic);
   const int j = u - r.head * p.head_units;
   r.pair = j < p.pair_units;
   r.at = r.pair ? j * 8 : p.pair_units * 16 + (j - p.pair_units) * 8;
@@ -76,7 +81,9 @@ __device__ __forceinline__ void store_cache(void* base, long long off, const flo
 
 template <bool F8>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams p) {
-  __shared__ float2 turn[128];  // cosine and sine of each pair
+  // cosine and sine of each pair, two pairs a vector: those of one unit (8 pairs, or 4 of pairs side by side) lie `units` apart, so that
+  // the units that a warp turns read neighbouring vectors
+  __shared__ float4 turn[64];
   __shared__ int sequence, position;
   __shared__ long long place;
   pdl_launch_dependents();
@@ -126,7 +133,8 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
     const double turns = (double)pos * (double)frequency * kTurnsPerRadian;
     float s, co;
     sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
-    turn[tid] = make_float2(co, s);
+    const int v = tid / 2, each = p.pair_units ? 4 : 2;
+    reinterpret_cast<float2*>(&turn[v % each * (p.rotary_dim / 4 / each) + v / each])[tid % 2] = make_float2(co, s);
   }
   __syncthreads();
 
@@ -140,19 +148,23 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
     if (r.pair) {
       to_floats(hi[i], y);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float2 cs = turn[r.at + j];
-        const float a = x[j], d = y[j];
+      for (int j = 0; j < 8; j += 2) {
+        const float4 cs = turn[j / 2 * p.pair_units + r.at / 8];
+        const float a = x[j], d = y[j], b = x[j + 1], e = y[j + 1];
         x[j] = a * cs.x - d * cs.y;
         y[j] = d * cs.x + a * cs.y;
+        x[j + 1] = b * cs.z - e * cs.w;
+        y[j + 1] = e * cs.z + b * cs.w;
       }
     } else if (r.turned) {
 #pragma unroll
-      for (int j = 0; j < 8; j += 2) {
-        const float2 cs = turn[(r.at + j) / 2];
-        const float a = x[j], d = x[j + 1];
+      for (int j = 0; j < 8; j += 4) {
+        const float4 cs = turn[j / 4 * (p.rotary_dim / 8) + r.at / 8];
+        const float a = x[j], d = x[j + 1], b = x[j + 2], e = x[j + 3];
         x[j] = a * cs.x - d * cs.y;
         x[j + 1] = d * cs.x + a * cs.y;
+        x[j + 2] = b * cs.z - e * cs.w;
+        x[j + 3] = e * cs.z + b * cs.w;
       }
     }
     if (r.head < p.q_heads) {
@@ -179,6 +191,8 @@ cudaError_t launch_kv_append(AppendParams p, int tokens, int interleaved, int sm
   p.rotary_dim = rotary;
   p.pair_units = interleaved ? 0 : rotary / 16;
   p.head_units = p.pair_units + (p.cache.head_dim - p.pair_units * 16) / 8;
+  p.head_magic = magic_of(p.head_units);
+  p.value_magic = magic_of(p.cache.head_dim / 8);
   p.units = (p.q_heads + p.cache.kv_heads) * p.head_units + p.cache.kv_heads * (p.cache.head_dim / 8);
   // a few tokens: their heads are spread over more CTAs, until the SMs have one each
   p.units_per_thread = kMostUnits;

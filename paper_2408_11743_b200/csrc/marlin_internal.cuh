@@ -141,6 +141,7 @@ struct AppendParams {
   int q_heads, rotary_dim;
   // filled in by the launch: units of a token, of a query or key head, of those its pairs; units that a thread takes
   int units, head_units, pair_units, units_per_thread;
+  uint32_t head_magic, value_magic;  // for divisions by head_units and by head_dim / 8 (kv_append.cu)
 };
 cudaError_t launch_kv_append(AppendParams p, int tokens, int interleaved, int sm_count, cudaStream_t stream);
 
