@@ -285,8 +285,10 @@ typedef struct {
  * and behind starts[sequences] belong to nobody: neither the cache nor their rows of the outputs are written.  A token whose position
  * would be negative (a sequence with fewer tokens than rows, for example an empty one of a padded batch) is not put
  * into the cache; its rows of the outputs are zeros.
- * A length outside of 0 .. max_pages * page_size (or 2^30, if that is less) is taken as the nearest of the two, a page number outside of 0 .. pages - 1 as a page
- * that is not there (nothing is written to it, attention reads zeros for it); both set the status word to MARLIN_ERR_CACHE. */
+ * A sequence whose length lies outside of 0 .. max_pages * page_size (or 2^30, if that is less) has no positions at all: its new
+ * tokens are not put into the cache, nothing is read for them, and their rows of the outputs are zeros.  A page number outside
+ * of 0 .. pages - 1 is a page that is not there (nothing is written to it, attention reads zeros for it).  Both set the status
+ * word to MARLIN_ERR_CACHE. */
 
 /* Bytes of workspace of the three calls below on heads of head_dim elements (0: not supported; host arithmetic only).
  * The workspace is that of marlin_workspace_bytes and under the same contract: zeroed once, the counters zero again

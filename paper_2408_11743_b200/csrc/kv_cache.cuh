@@ -11,13 +11,13 @@ __device__ __forceinline__ void report_cache(int* status) { atomicCAS(status, 0,
 
 constexpr int kLongest = 1 << 30;  // tokens of a sequence: positions, windows in front of them and tiles asked for ahead fit in 32 bits
 
-// Length of sequence b, kept inside of what its row of the table can hold.
+// Length of sequence b.  One that its row of the table cannot hold is reported and taken as 0, so that none of its new tokens has a
+// position: cut down to what the row holds, it would put them over tokens that are there already.
 __device__ __forceinline__ int cache_length(const KvCacheView& c, int b, int* status) {
   const int len = __ldg(c.lengths + b);
-  const long long most = min((long long)c.max_pages << c.page_shift, (long long)kLongest);
-  if (len < 0 || len > most) {
+  if (len < 0 || len > min((long long)c.max_pages << c.page_shift, (long long)kLongest)) {
     report_cache(status);
-    return len < 0 ? 0 : (int)most;
+    return 0;
   }
   return len;
 }

@@ -1,0 +1,74 @@
+"""The paged cache where calls reach its limits."""
+import numpy as np
+import pytest
+
+from cache_util import Case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def marlin():
+    import torch
+    assert torch.cuda.is_available()
+    import paper_2408_11743_b200 as m
+    m.lib()
+    return m
+
+
+def bits(x):
+    import torch
+    return x.view(torch.uint8)
+
+
+@pytest.mark.parametrize("length", [65, 67, 1000, 2 ** 30 + 1, 2 ** 31 - 1, -1, -2 ** 31])
+@pytest.mark.parametrize("new", [1, 5])
+@pytest.mark.parametrize("fill", ["pages of its own", "zeros"])
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_a_sequence_that_its_table_cannot_hold_has_no_place(marlin, length, new, fill, eight_bit):
+    # a row of four pages of 16 tokens, all of them valid (or filled up with page 0, which belongs to the other sequence)
+    import torch
+    case = Case([64, 49], new, 8, 2, 64, 16, eight_bit, seed=3)
+    d = case.dev(marlin)
+    table = torch.tensor([[3, 4, 5, 6], [0, 1, 2, 7]], dtype=torch.int32, device="cuda")
+    if fill == "zeros":
+        table[0, 1:] = 0
+    d["pages"] = table
+    inv = torch.from_numpy((10000.0 ** (-np.arange(32) / 32.0)).astype(np.float32)).cuda()
+    qkv = torch.from_numpy(case.qkv).cuda()
+    before = {name: d[name].clone() for name in ("k_cache", "v_cache")}
+    lone = {**d, **{name: x.clone() for name, x in before.items()}, "lengths": d["lengths"].clone()}
+    lone["lengths"][0] = 0  # what the other sequence has by itself
+    q_want = marlin.kv_append(qkv, **lone, inv_freq=inv)
+    o_want = marlin.attention_decode(q_want, **{k: x for k, x in lone.items()})
+    torch.cuda.synchronize()
+    assert marlin.read_status(lone["workspace"]) == 0
+
+    d["lengths"][0] = length
+    q = marlin.kv_append(qkv, **d, inv_freq=inv)
+    assert marlin.read_status(d["workspace"]) == 9
+    for name, x in before.items():
+        changed = (bits(d[name]) != bits(x)).view(x.shape[0], 2, 16, -1).any(-1).any(1).nonzero().tolist()
+        places = [(int(table[1, p // 16]), p % 16) for p in range(49 - new, 49)]
+        assert sorted(map(tuple, changed)) == sorted(places)  # the other sequence's new tokens alone
+        assert torch.equal(bits(d[name]), bits(lone[name]))
+    assert not q[:new].any() and torch.equal(q[new:], q_want[new:])
+    d["workspace"].zero_()
+    out = torch.full_like(q, 7.0)
+    marlin.attention_decode(q, **d, out=out)
+    assert marlin.read_status(d["workspace"]) == 9
+    assert not out[:new].any() and torch.equal(out[new:], o_want[new:])
+
+
+@pytest.mark.parametrize("length", [64, 63, 1, 0])
+def test_a_sequence_that_fills_its_table_is_as_any_other(marlin, length):
+    import torch
+    case = Case([length, 49], 1, 8, 2, 64, 16, seed=3, spare_pages=8)
+    d = case.dev(marlin)
+    d["pages"] = torch.tensor([[3, 4, 5, 6], [0, 1, 2, 7]], dtype=torch.int32, device="cuda")
+    qkv = torch.from_numpy(case.qkv).cuda()
+    marlin.kv_append(qkv, **d)
+    assert marlin.read_status(d["workspace"]) == 0
+    if length:
+        page = int(d["pages"][0, (length - 1) // 16])
+        assert torch.equal(d["k_cache"][page, :, (length - 1) % 16], qkv[0, 512:640].view(2, 64))
