@@ -636,10 +636,12 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         to_part += kLine;
       }
     };
+    // (lanes with and without an element of the head part in `give`, and meet again before the warp reads tensor memory as one)
     if (several && *(volatile int*)&sh.not_finite[odd]) {  // (one column at a time, with what was left out)
 #pragma unroll 1
       for (int r = mine; r < min(rows, mine + kMine); ++r) {
         float z;
+        __syncwarp();
         load_column(lanes + 2 * N + r, z);
         tc_wait_ld();
         give(r, z + not_finite_sum<G::F8>(p, x, sees, kTile, r, key));
@@ -648,6 +650,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
 #pragma unroll 1
       for (int r0 = mine; r0 < min(rows, mine + kMine); r0 += 8) {
         float z[8];
+        __syncwarp();
         load_columns(lanes + 2 * N + r0, z);
         tc_wait_ld();
 #pragma unroll

@@ -72,3 +72,28 @@ def test_a_sequence_that_fills_its_table_is_as_any_other(marlin, length):
     if length:
         page = int(d["pages"][0, (length - 1) // 16])
         assert torch.equal(d["k_cache"][page, :, (length - 1) % 16], qkv[0, 512:640].view(2, 64))
+
+
+@pytest.mark.parametrize("q_heads,dim", [(12, 16), (20, 48), (12, 80), (24, 112), (48, 80), (40, 16)])
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_values_that_are_not_finite_beside_lanes_without_an_element(marlin, q_heads, dim, eight_bit):
+    # several new tokens, one of whose values is NaN: rows that see it are summed up lane by lane, and heads that do not fill their
+    # tile leave some lanes out
+    import torch
+    case = Case([40, 300], [5, 3], q_heads, 1, dim, 16, eight_bit, seed=9)
+    d = case.dev(marlin)
+    q = torch.from_numpy(case.q.reshape(case.T, -1)).cuda()
+    want = marlin.attention_decode(q, **d).view(8, q_heads, dim).clone()
+    v = d["v_cache"].clone()
+    place = int(case.table[0][38 // 16]), 0, 38 % 16
+    if eight_bit:
+        v.view(torch.uint8)[place][dim - 1] = 0x7F
+    else:
+        v[place][dim - 1] = float("nan")
+    got = marlin.attention_decode(q, **{**d, "v_cache": v}).view(8, q_heads, dim)
+    torch.cuda.synchronize()
+    assert marlin.read_status(d["workspace"]) == 0
+    want[3:5, :, dim - 1] = float("nan")  # positions 38 and 39 of sequence 0
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    fine = ~torch.isnan(want)
+    assert torch.equal(got[fine], want[fine])
