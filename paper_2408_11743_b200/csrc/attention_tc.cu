@@ -76,6 +76,7 @@ struct TcShared {
   uint64_t opened[G::kOpen], closed[G::kOpen];
   uint64_t s_full[2], s_free[2];                       // logits are there; have been read
   uint64_t p_full[G::kPBuffers], p_done[G::kPBuffers]; // weights are there; have been multiplied
+  uint64_t drained[kIssuers];                          // all products of an issuing thread are complete
   Segment segments[G::kOpen];
   float2 ml[G::N];
   alignas(16) float base[G::N];  // of the rows, read four at a time; 0 where a row has seen nothing
@@ -411,6 +412,14 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
   }
 }
 
+// All products that this thread has issued are complete, and what they signal has arrived, before tensor memory is freed and the block's shared
+// memory goes to another: also where a wait ran out and nobody else has waited for them.  With a limit of its own (1 ms; a product takes
+// well below one microsecond), since the others do not wait any more then.
+__device__ __forceinline__ void drain_products(uint64_t* bar) {
+  tc_commit(bar);
+  for (int i = 0; i < 1000 && !mbar_try_wait(bar, 0); ++i) __nanosleep(1000);
+}
+
 // ---- softmax and results ---------------------------------------------------------------------------
 // Whether a wait has run out is agreed upon where a segment begins, so that these warps always meet at the same barriers; what
 // they compute of a segment whose copies did not come is thrown away with the call.
@@ -695,6 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
       mbar_init(&sh.p_full[i], kSoftmaxWarps);
       mbar_init(&sh.p_done[i], 1);
     }
+    for (int i = 0; i < kIssuers; ++i) mbar_init(&sh.drained[i], 1);
     sh.abort = 0;
     sh.not_finite[0] = sh.not_finite[1] = 0;
   }
@@ -720,10 +730,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
     const int w = warp - kSoftmaxWarps;
     if (w < kProducers)
       produce<G>(p, sh, w / 2, w % 2, ring, q_slots, ones + G::kOnes);
-    else if (w == kProducers && threadIdx.x % 32 == 0)
-      multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
-    else if (w == kProducers + 1 && threadIdx.x % 32 == 0)
-      multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
+    else if (w < kProducers + kIssuers && threadIdx.x % 32 == 0) {
+      if (w == kProducers)
+        multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
+      else
+        multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
+      drain_products(&sh.drained[w - kProducers]);
+    }
   }
   __syncwarp();
   tc_fence_before_sync();

@@ -87,3 +87,33 @@ def test_an_expired_wait_is_reported_and_the_next_call_is_correct(marlin, test_l
     ws2 = torch.zeros_like(ws)
     check(marlin.attention_decode(q, k, v, d["pages"], d["lengths"], ws2, scale=0.125, k_scale=d.get("k_scale"), v_scale=d.get("v_scale")))
     assert marlin.read_status(ws2) == 0
+
+
+@pytest.mark.parametrize("q_heads,dim,eight_bit", [(12, 64, False), (20, 48, False), (64, 64, False), (16, 112, False), (32, 128, False), (64, 80, True)])
+def test_products_that_are_under_way_when_a_wait_expires_end_before_the_block(marlin, test_lib, q_heads, dim, eight_bit):
+    # Every width of the tcgen05 kernel, three calls of it in a row that give up while products of earlier tiles may be running; calls on other
+    # workspaces, queued right behind them, use the same tensor memory and shared memory and have to be right.
+    import torch
+    from paper_2408_11743_b200 import binding
+    case = Case([200000, 700], 1, q_heads, 1, dim, 16, eight_bit, seed=q_heads)  # (worker 0 has more of it than an item costs beside its tiles)
+    d = case.dev(marlin)
+    q = torch.from_numpy(case.q.reshape(case.T, -1)).cuda()
+    k, v = d["k_cache"], d["v_cache"]
+    cache = binding.KvCache(
+        k=k.data_ptr(), v=v.data_ptr(), stride=(ctypes.c_int64 * 3)(*k.stride()[:3]), table=d["pages"].data_ptr(),
+        table_stride=d["pages"].stride(0), lengths=d["lengths"].data_ptr(),
+        k_scale=d["k_scale"].data_ptr() if eight_bit else None, v_scale=d["v_scale"].data_ptr() if eight_bit else None,
+        pages=case.pages, max_pages=d["pages"].shape[1], sequences=case.B, kv_heads=1, head_dim=dim, page_size=16, format=int(eight_bit))
+    stream = torch.cuda.current_stream().cuda_stream
+    spaces = [torch.zeros_like(d["workspace"]) for _ in range(6)]
+    outs = [torch.full_like(q, float("nan")) for _ in spaces]
+    for ws in spaces[::2]:
+        ws[:32].view(torch.int32)[7] = WITHHOLD_MAGIC
+    for ws, out in zip(spaces, outs):
+        assert test_lib.marlin_attention_decode(q.data_ptr(), q.stride(0), ctypes.byref(cache), None, case.T, q_heads, 0.125, 0,
+                                                out.data_ptr(), ws.data_ptr(), ws.numel(), stream) == 0
+    ref = case.attention_ref(0.125)
+    for i, (ws, out) in enumerate(zip(spaces, outs)):
+        assert test_lib.marlin_read_status(ws.data_ptr(), stream) == (0 if i % 2 else 8)
+        if i % 2:
+            assert np.all(np.abs(out.float().cpu().numpy().reshape(ref[0].shape) - ref[0]) <= attention_bound(ref))
