@@ -143,7 +143,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
     // one tile and of the next one.  INT_MIN where no key is asked for
     auto page_of = [&](int i) {
       const int key = key_first + (big_pages ? i + lane : i) * kTile + (big_pages ? 0 : lane & 15);
-      return x.nt > 0 && key < high && key + (big_pages ? 16 : 1) > low ? __ldg(table + (key >> c.page_shift)) : INT_MIN;
+      return x.nt > 0 && key < high && key + (big_pages ? 16 : 1) > low ? load(table + (key >> c.page_shift)) : INT_MIN;
     };
     const int batch = big_pages ? 32 : 1;
     const long long head_bytes = (x.h * c.s_head + my_row * c.s_token) * kElement + my_vec * 16;
@@ -260,7 +260,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         high[j][i] = several ? x.base_high + (x.row0 + min(rows - 1, wm * 8 * NT + j * 8 + t4 * 2 + i)) / p.group : high_min;
-    const float factor = p.scale_log2 * (F8 && c.k_scale ? __ldg(c.k_scale + x.h) : 1.f);
+    const float factor = p.scale_log2 * (F8 && c.k_scale ? load(c.k_scale + x.h) : 1.f);
 
     // operands of Q: rows on the 8-wide side; of 16 elements a thread has 2 t, 2 t + 1, 2 t + 8, 2 t + 9, or, to match the
     // bytes of an 8-bit key, 4 t .. 4 t + 3

@@ -104,13 +104,13 @@ __device__ __forceinline__ void prefetch_table(const AttentionParams& p, int thr
 struct Sequence {
   int len, n, first, tile0, tiles, blocks;
 };
-__device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, int rows, int tile) {
+__device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, int rows, int tile, bool& bad) {
   Sequence s;
-  s.len = cache_length(p.cache, b, p.status);
+  s.len = cache_length(p.cache, b, bad);
   s.first = b;
   s.n = 1;
   if (p.starts) {
-    const int from = min(max(__ldg(p.starts + b), 0), p.tokens), to = min(max(__ldg(p.starts + b + 1), from), p.tokens);
+    const int from = min(max(load(p.starts + b), 0), p.tokens), to = min(max(load(p.starts + b + 1), from), p.tokens);
     s.first = from;
     s.n = to - from;
   }
@@ -178,11 +178,13 @@ struct Range {
     // lane i counts the tiles of sequences [i * per, (i + 1) * per)
     const int per = (c.sequences + 31) / 32;
     uint32_t mine = 0;
+    bool bad = false;
     for (int i = lane * per; i < min(c.sequences, (lane + 1) * per); ++i) {
-      const Sequence s = sequence(p, i, ROWS, TILE);
+      const Sequence s = sequence(p, i, ROWS, TILE, bad);
       const unsigned long long units = (unsigned long long)c.kv_heads * s.blocks * (s.tiles + LEAD) + mine;
       mine = (uint32_t)min(units, (unsigned long long)kMostUnits);
     }
+    if (bad) report_cache(p.status);
     uint32_t before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -211,7 +213,7 @@ struct Range {
       b = owner * per;
       uint32_t off = at - __shfl_sync(~0u, before, owner);
       for (;; ++b) {
-        s = sequence(p, b, ROWS, TILE);
+        s = sequence(p, b, ROWS, TILE, bad);
         const uint32_t units = (uint32_t)c.kv_heads * s.blocks * (s.tiles + LEAD);
         if (off < units) break;
         off -= units;
@@ -234,7 +236,8 @@ struct Range {
         skip = 0;
         if (++item == c.kv_heads * s.blocks) {
           item = 0;
-          do s = sequence(p, ++b, ROWS, TILE);
+          bool bad = false;  // (reported by begin())
+          do s = sequence(p, ++b, ROWS, TILE, bad);
           while (s.blocks == 0);
         }
       }
@@ -278,7 +281,7 @@ __device__ __forceinline__ int token_of(const AttentionParams& p, const Segment&
 __device__ __forceinline__ void write_four(const AttentionParams& p, const Segment& x, int r, int d, float4 z, float li) {
   const int token = token_of(p, x, r), head = x.h * p.group + x.row0 + r - token * p.group;
   const bool nothing = x.base_high + token <= 0;
-  const float f = nothing ? 0.f : (p.cache.v_scale ? __ldg(p.cache.v_scale + x.h) : 1.f) / li;
+  const float f = nothing ? 0.f : (p.cache.v_scale ? load(p.cache.v_scale + x.h) : 1.f) / li;
   if (nothing) z = make_float4(0.f, 0.f, 0.f, 0.f);
   uint2 two;
   two.x = half2_bits(z.x * f, z.y * f);
@@ -300,7 +303,7 @@ __device__ __forceinline__ float not_finite_sum(const AttentionParams& p, const 
       pos = sees.high_min - 1;
       continue;
     }
-    const long long off = cache_offset(c, __ldg(c.table + x.b * c.table_stride + (pos >> c.page_shift)), x.h, pos, p.status);
+    const long long off = cache_offset(c, load(c.table + x.b * c.table_stride + (pos >> c.page_shift)), x.h, pos, p.status);
     if (off < 0) continue;
     float v;
     if (F8) {

@@ -199,7 +199,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
     auto key_of = [&](int i) { return key_first + (i + lane / 4) * kTile + lane % 4 * 16; };
     auto page_of = [&](int i) {
       const int key = key_of(i);
-      return big_pages && x.nt > 0 && key < high && key + 16 > low ? __ldg(table + (key >> c.page_shift)) : -1;
+      return big_pages && x.nt > 0 && key < high && key + 16 > low ? load(table + (key >> c.page_shift)) : -1;
     };
     auto place_of = [&](int i, int page) {
       return (unsigned)page < (unsigned)c.pages
@@ -252,7 +252,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
             for (int j = 0; j < kPasses; ++j) {
               const int key = key0 + j * kPer8 + row8;
               const bool asked = key >= low && key < high;
-              const long long at = asked ? cache_offset(c, __ldg(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
+              const long long at = asked ? cache_offset(c, load(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
               copy16(to + j * 512, cache + (at >= 0 && part8 ? at + vec8 * 16 : 0), at >= 0 && part8);
             }
           }
@@ -328,7 +328,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
           for (int r = 0; r < 64; r += kPer) {
             const int row = r + my_row, key = key0 + row;
             const bool asked = key >= low && key < high;
-            const long long at = asked ? cache_offset(c, __ldg(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
+            const long long at = asked ? cache_offset(c, load(table + (key >> c.page_shift)), x.h, key, p.status) : -1;
             const bool there = at >= 0 && my_part;
             copy16(to + r * 128 + ((my_vec ^ row) & 7) * 16, cache + (there ? at * 2 + my_vec * 16 : 0), there);
           }
@@ -455,7 +455,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       meet_half();
     }
     bool fresh = true;  // some row has not seen a key yet
-    const float scale = p.scale_log2 * (G::F8 && c.k_scale ? __ldg(c.k_scale + x.h) : 1.f);
+    const float scale = p.scale_log2 * (G::F8 && c.k_scale ? load(c.k_scale + x.h) : 1.f);
     // (a hidden logit is an infinity, and would not stay one under 0: products of finite numbers times 1e-30 have weights of 1 all the same)
     const float factor = scale == 0.f ? 1e-30f : scale, hidden = factor < 0.f ? INFINITY : -INFINITY;
     float l[kMine];     // (kSumRows: not used)
@@ -627,7 +627,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     uint16_t* to_out = p.out + ((long long)(x.first + token) * p.q_heads + x.h * p.group + head) * c.head_dim + key;
     float* to_part = part_of(p, x, blockIdx.x, N, DP) + mine * kLine;
     const int next_token = (p.q_heads - p.group) * c.head_dim;
-    const float values_of = G::F8 && c.v_scale ? __ldg(c.v_scale + x.h) : 1.f;
+    const float values_of = G::F8 && c.v_scale ? load(c.v_scale + x.h) : 1.f;
     auto give = [&](int r, float z) {
       const float sum = sh.alpha[r];
       if (whole) {

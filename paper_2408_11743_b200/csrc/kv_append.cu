@@ -105,23 +105,25 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
       src = p.k + (long long)t * p.k_stride + (r.head - p.q_heads) * c.head_dim;
     else
       src = p.v + (long long)t * p.v_stride + (r.head - p.q_heads - c.kv_heads) * c.head_dim;
-    lo[i] = __ldg(reinterpret_cast<const uint4*>(src + r.at));
-    if (r.pair) hi[i] = __ldg(reinterpret_cast<const uint4*>(src + r.at + p.rotary_dim / 2));
+    lo[i] = load(reinterpret_cast<const uint4*>(src + r.at));
+    if (r.pair) hi[i] = load(reinterpret_cast<const uint4*>(src + r.at + p.rotary_dim / 2));
   }
 
   // whose token this is, and where it goes: every thread looks at a sequence, and the one whose rows hold the token follows the
   // table, so that the loads of a step are on their way together
-  const float frequency = p.inv_freq && tid < p.rotary_dim / 2 ? __ldg(p.inv_freq + tid) : 0.f;
+  const float frequency = p.inv_freq && tid < p.rotary_dim / 2 ? load(p.inv_freq + tid) : 0.f;
   if (tid == 0) sequence = -1;
   __syncthreads();
   for (int b = p.starts ? tid : t; b < (p.starts ? c.sequences : t + 1); b += kThreads) {
     if (!p.starts && tid > 0) break;
-    const int from = p.starts ? __ldg(p.starts + b) : t, end = p.starts ? __ldg(p.starts + b + 1) : t + 1;
-    const int len = cache_length(c, b, p.status);
+    const int from = p.starts ? load(p.starts + b) : t, end = p.starts ? load(p.starts + b + 1) : t + 1;
+    bool bad = false;
+    const int len = cache_length(c, b, bad);
+    if (bad) report_cache(p.status);
     if (from > t || t >= end) continue;
     const int pos = len - (end - t);
     position = pos;
-    place = pos >= 0 ? cache_offset(c, __ldg(c.table + b * c.table_stride + (pos >> c.page_shift)), 0, pos, p.status) : -1;
+    place = pos >= 0 ? cache_offset(c, load(c.table + b * c.table_stride + (pos >> c.page_shift)), 0, pos, p.status) : -1;
     sequence = b;
   }
   __syncthreads();
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
       const bool key = r.head < p.q_heads + c.kv_heads;
       const int h = r.head - p.q_heads - (key ? 0 : c.kv_heads);
       const float* scales = key ? c.k_scale : c.v_scale;
-      const float scale = F8 && scales ? __ldg(scales + h) : 1.f;
+      const float scale = F8 && scales ? load(scales + h) : 1.f;
       const long long off = to + h * c.s_head + r.at;
       store_cache<F8>(key ? c.k : c.v, off, x, scale);
       if (r.pair) store_cache<F8>(key ? c.k : c.v, off + p.rotary_dim / 2, y, scale);

@@ -6,20 +6,39 @@
 
 namespace marlin_b200 {
 
+// These kernels start while the one before them in the stream still runs, and wait for its end (pdl_wait_prior_grids) before they read
+// anything: what it writes, such as the output of the qkv layer, lengths or a page table, changes while they live.  A load through the
+// read-only path (__ldg, ld.global.nc) is for memory that nobody writes during the whole kernel, and may be moved in front of the wait; these
+// are ordinary loads, which the compiler keeps behind it, in their order, but is free to move over stores.
+__device__ __forceinline__ int load(const int* p) {
+  int x;
+  asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(p));
+  return x;
+}
+__device__ __forceinline__ float load(const float* p) {
+  float x;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(x) : "l"(p));
+  return x;
+}
+__device__ __forceinline__ uint4 load(const uint4* p) {
+  uint4 x;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+  return x;
+}
+
 // The first report of a call that reaches outside of the cache; a time-out that is already there stays.
 __device__ __forceinline__ void report_cache(int* status) { atomicCAS(status, 0, (int)MARLIN_ERR_CACHE); }
 
 constexpr int kLongest = 1 << 30;  // tokens of a sequence: positions, windows in front of them and tiles asked for ahead fit in 32 bits
 
-// Length of sequence b.  One that its row of the table cannot hold is reported and taken as 0, so that none of its new tokens has a
+// Length of sequence b.  One that its row of the table cannot hold is bad and taken as 0, so that none of its new tokens has a
 // position: cut down to what the row holds, it would put them over tokens that are there already.
-__device__ __forceinline__ int cache_length(const KvCacheView& c, int b, int* status) {
-  const int len = __ldg(c.lengths + b);
-  if (len < 0 || len > min((long long)c.max_pages << c.page_shift, (long long)kLongest)) {
-    report_cache(status);
-    return 0;
-  }
-  return len;
+// (`bad` is for the caller to report, behind the loads of other sequences, which an atomic in between would hold back.)
+__device__ __forceinline__ int cache_length(const KvCacheView& c, int b, bool& bad) {
+  const int len = load(c.lengths + b);
+  const bool fits = len >= 0 && len <= min((long long)c.max_pages << c.page_shift, (long long)kLongest);
+  bad |= !fits;
+  return fits ? len : 0;
 }
 
 // Offset (in elements) of the token at position pos < max_pages * page_size, head h; -1 where its page is not there.

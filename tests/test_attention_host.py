@@ -163,3 +163,14 @@ def test_the_oracle_is_softmax_attention_on_a_plain_layout(marlin):
         assert np.allclose([y[0, i], y[0, j]], [x[0, i] * np.cos(1.5) - x[0, j] * np.sin(1.5), x[0, j] * np.cos(1.5) + x[0, i] * np.sin(1.5)])
         assert np.array_equal(y[0, 4:], x[0, 4:])
         assert np.allclose((y ** 2).sum(), (x ** 2).sum())
+
+
+def test_the_kernels_read_nothing_through_the_read_only_path():
+    # they are resident while the kernel before them still writes what they read
+    import os
+    from paper_2408_11743_b200 import build
+    for name in ("kv_append.cu", "kv_cache.cuh", "attention.cu", "attention.cuh", "attention_tc.cu"):
+        with open(os.path.join(build.CSRC, name)) as f:
+            code = "\n".join(line.split("//")[0] for line in f)
+        for word in ("__ldg", "ld.global.nc", "__restrict__"):
+            assert word not in code, (name, word)
