@@ -650,21 +650,21 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
 #pragma unroll 1
       for (int r = mine; r < min(rows, mine + kMine); ++r) {
         float z;
-        __syncwarp();
         load_column(lanes + 2 * N + r, z);
         tc_wait_ld();
         give(r, z + not_finite_sum<G::F8>(p, x, sees, kTile, r, key));
+        __syncwarp();
       }
     } else {
 #pragma unroll 1
       for (int r0 = mine; r0 < min(rows, mine + kMine); r0 += 8) {
         float z[8];
-        __syncwarp();
         load_columns(lanes + 2 * N + r0, z);
         tc_wait_ld();
 #pragma unroll
         for (int r = 0; r < 8; ++r)
           if (r0 + r < rows) give(r0 + r, z[r]);
+        __syncwarp();
       }
     }
     tc_fence_before_sync();
