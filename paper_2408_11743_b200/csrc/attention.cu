@@ -379,7 +379,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
             const float old = m[j][i] == kNone ? 0.f : m[j][i];
-            const float now = fmaxf(m[j][i], top + old);
+            const float now = fmaxf(m[j][i], top + old - kBelow);
             const float base = now == kNone ? 0.f : now;
             const float alpha = exp2_fast(m[j][i] - base), shift = old - base;
             m[j][i] = now;
@@ -396,8 +396,7 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
         open = __any_sync(~0u, none);
       }
 
-      // weights, rounded to fp16 for the product (2^-11 of each at most, or 2^-25 of the largest), and turned round: keys on the
-      // side that is summed over
+      // weights, rounded to fp16 for the product (kBelow in attention.cuh), and turned round: keys on the side that is summed over
       uint32_t w[NT][2];
 #pragma unroll
       for (int j = 0; j < NT; ++j) {

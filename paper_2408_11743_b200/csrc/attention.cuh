@@ -13,10 +13,14 @@ constexpr int kItemCounters = 2 * kMostCtas;  // counters of items behind those 
 static_assert(3 * kMostCtas * sizeof(int) <= kWsPartialOff - kWsCounterOff, "counters");
 constexpr int kGroup = 8;  // parts that are joined at once; more of them are joined in groups first, each by its last CTA
 constexpr float kNone = -INFINITY;
-// A row's sums are kept relative to 2^base, base its largest logit (in units of log2) when the base was last moved.  It moves only
-// when a logit exceeds it by more than this, so that most tiles neither look for a maximum across lanes nor rescale:
-// weights are then at most 2^8, far from the end of fp16, and their rounding is relative.
-constexpr float kSlack = 8.f;
+// A row's sums are kept relative to 2^base, base its largest logit (in units of log2) when the base was last moved, less kBelow.  It moves
+// only when a logit exceeds it by more than kSlack, so that most tiles neither look for a maximum across lanes nor rescale.
+// Weights are then at most 2^15 (fp16 ends at 2^16), and the largest of a row at least 2^7.  They are rounded to fp16 for the product
+// with the values, the only operand type in which that product takes values as they lie in the cache: by 2^-11 of themselves at
+// most, or by 2^-25 where they are below 2^-14.  So what a weight loses is at most 2^-11 of it or 2^-32 of the largest: a million
+// keys far below one large one lose 2^-12 of the whole.  (Without kBelow, which costs nothing, they would lose 2^-5.)
+constexpr float kBelow = 7.f;
+constexpr float kSlack = 15.f;
 
 constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 

@@ -80,7 +80,7 @@ struct TcShared {
   Segment segments[G::kOpen];
   float2 ml[G::N];
   alignas(16) float base[G::N];  // of the rows, read four at a time; 0 where a row has seen nothing
-  float largest[G::N];           // the same, -inf where a row has seen nothing
+  float largest[G::N];           // the same, -inf where a row has seen nothing (its largest logit less kBelow)
   float alpha[G::N];             // what the sums are multiplied with when the base moves
   float tops[4][G::N];           // of the warps: largest logits; sums of weights
   int high[G::N];                // positions below which the rows see
@@ -488,7 +488,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         for (int r = 0; r < kMine; r += 4) {
           // (row r + warp % 4, without an index that is not known to the compiler)
           const float z = (warp & 2) ? ((warp & 1) ? y[r + 3] : y[r + 2]) : ((warp & 1) ? y[r + 1] : y[r]);
-          const float top = warp_max(z == hidden ? kNone : z * factor);
+          const float top = warp_max(z == hidden ? kNone : z * factor) - kBelow;
           none |= top == kNone;
           if (lane == 0) {
             sh.largest[mine + r + (warp & 3)] = top;
@@ -518,7 +518,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         meet_half();
         for (int r = mine + key; r < mine + kMine; r += 128) {
           const float old = sh.largest[r], from = sh.base[r];
-          const float top = fmaxf(fmaxf(sh.tops[0][r], sh.tops[1][r]), fmaxf(sh.tops[2][r], sh.tops[3][r])) + from;
+          const float top = fmaxf(fmaxf(sh.tops[0][r], sh.tops[1][r]), fmaxf(sh.tops[2][r], sh.tops[3][r])) + from - kBelow;
           const float now = fmaxf(old, top), to = now == kNone ? 0.f : now;
           sh.alpha[r] = exp2_fast(old - to);
           sh.tops[0][r] = from - to;
@@ -551,7 +551,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         }
         meet_half();  // (alpha and tops are free again)
       }
-      // weights, rounded to fp16 for the product (2^-11 of each at most, or 2^-25 of the largest)
+      // weights, rounded to fp16 for the product (kBelow in attention.cuh)
       wait(&sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1);  // (those that were there are multiplied)
       const uint32_t w_to = weights + pb * G::kPBytes + key * G::kPRow;
 #pragma unroll

@@ -97,3 +97,31 @@ def test_values_that_are_not_finite_beside_lanes_without_an_element(marlin, q_he
     assert torch.equal(torch.isnan(got), torch.isnan(want))
     fine = ~torch.isnan(want)
     assert torch.equal(got[fine], want[fine])
+
+
+@pytest.mark.parametrize("q_heads,dim", [(1, 64), (8, 128), (16, 64), (16, 128), (40, 64), (40, 128), (8, 256), (40, 256)])
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_many_weights_far_below_the_largest(marlin, q_heads, dim, eight_bit):
+    # Sixteen keys have a weight of 1 and the value 0, 131056 others one of 2^-26 and the value 256: the others have 2^-13 of the weights
+    # together, and make all of the result, 2^-13 * 256.  (Every warp that multiplies has one of the sixteen.)
+    # A weight of 2^-26 of the largest has to survive its rounding to fp16.  All weights are powers of two: what is left is the rounding
+    # of the logit (26 to 2^-19 of it in base 2, so 2^-14 of a weight at most), sums in fp32 of equal terms, the sum of the weights,
+    # where the small ones may be lost beside a large one (2^-13 of it), and the result's rounding.
+    import torch
+    n, page, sequences = 1 << 17, 1 << 10, 320   # (more items than CTAs: no CTA has few of their keys)
+    kind = torch.float8_e4m3fn if eight_bit else torch.float16
+    k = torch.zeros(n // page, 1, page, dim, device="cuda")
+    v = torch.full_like(k, 256.0)
+    k[0, 0, 0:256:16, 0] = 13.0
+    v[0, 0, 0:256:16] = 0.0
+    q = torch.zeros(sequences, q_heads, dim, dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 2.0
+    table = torch.arange(n // page, dtype=torch.int32, device="cuda").repeat(sequences, 1)
+    lengths = torch.full((sequences,), n, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(marlin.attention_workspace_bytes(dim), dtype=torch.uint8, device="cuda")
+    out = marlin.attention_decode(q.view(sequences, -1), k.to(kind), v.to(kind), table, lengths, ws, scale=float(np.float32(np.log(2.0))))
+    assert marlin.read_status(ws) == 0
+    rest = (n - 16) * np.exp(-26.0 * float(np.float32(np.log(2.0))))
+    want = 256.0 * rest / (16.0 + rest)
+    off = (out.double() - want).abs().max().item()
+    assert off <= want * (2.0 ** -11 + 2.0 ** -14 + 2.0 ** -13 + 2.0 ** -18), (off, want)
