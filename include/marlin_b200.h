@@ -347,7 +347,8 @@ MARLIN_API int marlin_attention_block(const void* A, const void* w_qkv, const vo
 /* Synchronises `stream`, then returns the device-side status word of `workspace`
  * (MARLIN_OK, MARLIN_ERR_DEVICE_TIMEOUT if a kernel gave up a bounded wait, or MARLIN_ERR_CACHE), or
  * MARLIN_ERR_CUDA if the stream reports an error.  The status word is sticky until the
- * workspace is zeroed again. */
+ * workspace is zeroed again.  Where there have been both, it is MARLIN_ERR_DEVICE_TIMEOUT: results of that call and the counters
+ * are not to be relied on, while MARLIN_ERR_CACHE says that some tokens were left out and all else is right. */
 MARLIN_API int marlin_read_status(const void* workspace, marlin_stream stream);
 
 /* ---- host-side planning, exposed for inspection and tests (no GPU needed) ----------------------- */

@@ -106,7 +106,7 @@ size_t marlin_packed_meta_bytes(int K, int N) {
   return (size_t)K * N / 8;
 }
 
-// Workspace map: [status word, counters: 8192 bytes][partial-tile slots].  The counters are zero at rest and every kernel
+// Workspace map: [status words, counters: 8192 bytes][partial-tile slots].  The counters are zero at rest and every kernel
 // leaves them that way; the slots are written before they are read in every call, and what they hold in between means
 // nothing (the tcgen05 kernel clears most of what it has read, the others leave it).
 // So one buffer may serve calls on different layers, batch sizes and formats one after the other.
@@ -614,13 +614,13 @@ int marlin_attention_block(const void* A, const void* w_qkv, const void* s_qkv, 
 
 int marlin_read_status(const void* workspace, marlin_stream stream) {
   if (!workspace) return MARLIN_ERR_NULL;
-  int host_status = 0;
+  int words[kWsCacheWord + 1] = {};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (cudaMemcpyAsync(&host_status, static_cast<const uint8_t*>(workspace) + kWsStatusOff, sizeof(int),
-                      cudaMemcpyDeviceToHost, s) != cudaSuccess)
+  if (cudaMemcpyAsync(words, static_cast<const uint8_t*>(workspace) + kWsStatusOff, sizeof(words), cudaMemcpyDeviceToHost, s) !=
+      cudaSuccess)
     return MARLIN_ERR_CUDA;
   if (cudaStreamSynchronize(s) != cudaSuccess) return MARLIN_ERR_CUDA;
-  return host_status;
+  return words[0] ? words[0] : words[kWsCacheWord];  // a wait that ran out is the graver of the two
 }
 
 int marlin_plan_stripes(int M, int K, int N, int sm_count, int* n_tile, int* workers, int64_t* bounds, int cap) {

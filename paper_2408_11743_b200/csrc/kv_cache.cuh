@@ -26,8 +26,9 @@ __device__ __forceinline__ uint4 load(const uint4* p) {
   return x;
 }
 
-// The first report of a call that reaches outside of the cache; a time-out that is already there stays.
-__device__ __forceinline__ void report_cache(int* status) { atomicCAS(status, 0, (int)MARLIN_ERR_CACHE); }
+// A call that reaches outside of the cache says so in a word of its own: a wait that runs out, there or in a later call on the workspace,
+// finds the status word free, and neither hides the other.  (Any number of threads write the same.)
+__device__ __forceinline__ void report_cache(int* status) { *(volatile int*)(status + kWsCacheWord) = MARLIN_ERR_CACHE; }
 
 constexpr int kLongest = 1 << 30;  // tokens of a sequence: positions, windows in front of them and tiles asked for ahead fit in 32 bits
 

@@ -30,7 +30,8 @@ constexpr int kMaxSlabM = 16;         // rows of A handled by one launch of the 
 constexpr int kSmemBudget = 227 * 1024;
 
 // workspace layout (bytes)
-constexpr size_t kWsStatusOff = 0;
+constexpr size_t kWsStatusOff = 0;    // what the waits report: a status and a record behind it, eight words
+constexpr int kWsCacheWord = 8;       // behind them: what the kernels of the paged cache report of lengths and page numbers
 constexpr size_t kWsCounterOff = 256;
 constexpr int kWsMaxCounters = 1024;  // N / 64 <= 1024
 constexpr size_t kWsPartialOff = 8192;

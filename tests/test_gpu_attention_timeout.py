@@ -117,3 +117,40 @@ def test_products_that_are_under_way_when_a_wait_expires_end_before_the_block(ma
         assert test_lib.marlin_read_status(ws.data_ptr(), stream) == (0 if i % 2 else 8)
         if i % 2:
             assert np.all(np.abs(out.float().cpu().numpy().reshape(ref[0].shape) - ref[0]) <= attention_bound(ref))
+
+
+def test_a_time_out_and_a_report_of_the_cache_do_not_hide_each_other(marlin, test_lib):
+    # a page that is not there is reported and contained; a wait that expires later, on the same workspace, is what the host has to know
+    import torch
+    from paper_2408_11743_b200 import binding
+    case = Case([130000], 1, 4, 1, 128, 16, seed=1)
+    d = case.dev(marlin)
+    q = torch.from_numpy(case.q.reshape(case.T, -1)).cuda()
+    out = torch.zeros_like(q)
+    ws = d["workspace"]
+    stream = torch.cuda.current_stream().cuda_stream
+    k, v, good = d["k_cache"], d["v_cache"], d["pages"]
+    bad = good.clone()
+    bad[0, 5] = case.pages
+
+    def call(table):
+        cache = binding.KvCache(
+            k=k.data_ptr(), v=v.data_ptr(), stride=(ctypes.c_int64 * 3)(*k.stride()[:3]), table=table.data_ptr(),
+            table_stride=table.stride(0), lengths=d["lengths"].data_ptr(), pages=case.pages, max_pages=table.shape[1], sequences=1,
+            kv_heads=1, head_dim=128, page_size=16, format=0)
+        assert test_lib.marlin_attention_decode(q.data_ptr(), q.stride(0), ctypes.byref(cache), None, 1, 4, 0.125, 0, out.data_ptr(),
+                                                ws.data_ptr(), ws.numel(), stream) == 0
+        return test_lib.marlin_read_status(ws.data_ptr(), stream)
+
+    assert call(good) == 0
+    assert call(bad) == 9
+    assert call(good) == 9  # it stays until the workspace is zeroed
+    ws[:32].view(torch.int32)[7] = WITHHOLD_MAGIC
+    assert call(good) == 8
+    rec = ws[:32].cpu().numpy().view(np.int32)
+    assert rec[0] == 8 and rec[1] == 0 and rec[6] >= 4000  # with its record
+    ws.zero_()
+    ws[:32].view(torch.int32)[7] = WITHHOLD_MAGIC
+    assert call(bad) == 8  # both in one call
+    ws.zero_()
+    assert call(good) == 0
