@@ -125,3 +125,41 @@ def test_many_weights_far_below_the_largest(marlin, q_heads, dim, eight_bit):
     want = 256.0 * rest / (16.0 + rest)
     off = (out.double() - want).abs().max().item()
     assert off <= want * (2.0 ** -11 + 2.0 ** -14 + 2.0 ** -13 + 2.0 ** -18), (off, want)
+
+
+@pytest.mark.parametrize("q_heads,kv_heads,sequences,length", [(64, 64, 4096, 1 << 20), (192, 16, 1024, 1 << 23)])
+def test_more_tiles_than_32_bits_count(marlin, q_heads, kv_heads, sequences, length):
+    # 2^32 tiles of 64 keys with a row each, and 2^30 of 128 keys with 12 rows on the tensor cores' fifth generation (two to four seconds
+    # each).  All entries of the table are page 0 but the last of every row, page 1, so that the result is that of two pages, the first
+    # counted as often as it is there.
+    import torch
+    page, dim = 1 << 14, 16
+    times = length // page - 1
+    gen = torch.Generator(device="cuda").manual_seed(q_heads)
+    k, v = (torch.randn(2, kv_heads, page, dim, generator=gen, device="cuda", dtype=torch.float16) for _ in "kv")
+    v[1] += 64.0
+    q = torch.randn(sequences, q_heads * dim, generator=gen, device="cuda", dtype=torch.float16)
+    table = torch.zeros(sequences, length // page, dtype=torch.int32, device="cuda")
+    table[:, -1] = 1
+    lengths = torch.full((sequences,), length, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(marlin.attention_workspace_bytes(dim), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, float("nan"))
+    marlin.attention_decode(q, k, v, table, lengths, ws, scale=0.25, out=out)
+    assert marlin.read_status(ws) == 0
+    group = q_heads // kv_heads
+    # A sum of one warp (or of one CTA on tcgen05, 16 keys at a time) is added up in fp32 over at most length / 16 steps, each off by
+    # 2^-24 of the sum so far: all sums have one sign in the weights and are bounded by the spread in the values; numerator and
+    # denominator: 2 * length / 16 * 2^-24.  The rest as in cache_util.attention_bound, with |logit| <= 16 |q| |k| * 0.25 < 64.
+    relative = 2.0 ** -11 + 2.0 ** -20 + 2 * length / 16 * 2.0 ** -24 + 4 * 32 * 2.0 ** -24 * 64
+    times = torch.tensor([times, 1], dtype=torch.float64, device="cuda").repeat_interleave(page)
+    for h in range(kv_heads):
+        rows = q.view(sequences, kv_heads, group, dim)[:, h].reshape(-1, dim).double()
+        got = out.view(sequences, kv_heads, group, dim)[:, h].reshape(-1, dim).double()
+        keys, values = k[:, h].reshape(-1, dim).double(), v[:, h].reshape(-1, dim).double()
+        for a in range(0, len(rows), 4096):
+            s = rows[a:a + 4096] @ keys.T * 0.25
+            w = (s - s.amax(-1, keepdim=True)).exp() * times
+            w /= w.sum(-1, keepdim=True)
+            want, spread = w @ values, w @ values.abs()
+            off = (got[a:a + 4096] - want).abs()
+            assert bool((off <= 2.0 ** -11 * want.abs() + relative * spread).all())  # (false for NaN)
