@@ -324,8 +324,9 @@ MARLIN_API int marlin_kv_append(const void* q, int64_t q_stride, const void* k, 
  * last, in the order of the keys, so that the same inputs give the same bits on every call.  Sums and the softmax are fp32;
  * a weight is rounded to fp16 before it is multiplied with a value: by at most 2^-11 of it, or 2^-32 of the largest weight of its
  * row if that is more.  One below that counts as 0 there (n such keys are missing from the result by up to n 2^-32 of the weights,
- * and an infinite value under such a weight gives NaN).  A call that
- * has more than 2^29 tiles for each of its CTAs (minutes of work) is refused on the device (MARLIN_ERR_CACHE, nothing is written).
+ * and an infinite value under such a weight gives NaN).  A call of
+ * 2^32 tiles or more (an item counts for two to four beside its own; 40 s of work with heads of 128 elements) is refused
+ * on the device (MARLIN_ERR_CACHE, nothing is written).
  * Any number of tokens per sequence is right; it is made for one and the few of speculative decoding (bound by reading the cache). */
 MARLIN_API int marlin_attention_decode(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const int32_t* starts,
                             int tokens, int q_heads, float scale, int window, void* out,

@@ -7,7 +7,7 @@
 namespace marlin_b200 {
 
 constexpr int kLeastTiles = 4;  // units that a CTA takes at least, where there are fewer than CTAs would like
-constexpr uint32_t kMostUnits = 1u << 29;  // of one CTA
+constexpr uint32_t kMostUnits = 0xffffffffu;  // of a call, and more than it can have: sums that reach it stay there
 constexpr int kMostCtas = kMaxWorkers;
 constexpr int kItemCounters = 2 * kMostCtas;  // counters of items behind those of groups
 static_assert(3 * kMostCtas * sizeof(int) <= kWsPartialOff - kWsCounterOff, "counters");
@@ -129,28 +129,15 @@ __device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, in
 // late.  Worker w of W begins at unit w * (U / W) + min(w, U % W).  A range that would begin within the lead, or within `snap` tiles of
 // the beginning or the end of an item, begins there instead: a part of an item costs a round trip through the workspace, which
 // is worth a tile or two where a CTA has few.
-// There may be more units than 32 bits count (16 prompts of 131072 tokens with 32 key heads are 2^30 tiles of 128 keys, some seconds of work).  A
-// CTA therefore counts from the beginning of its own range, in 32 bits: an item has at most 2^25 + LEAD units (kLongest keys in tiles of
-// 32), and what the CTA looks at are the items of its range, of at most kMostUnits, and the boundaries inside of them.
-// (Divisions of 64 bits are a routine that costs the warps that follow a range their registers, so there are none.)
-using Units = unsigned long long;
 struct Stripes {
-  uint32_t workers, size, more;
-  int snap, lead;
-  __device__ __forceinline__ Units origin(uint32_t w) const { return (Units)w * size + min(w, more); }
-  // where the range of worker w begins, before any move, from where this one does
-  __device__ __forceinline__ int begin(uint32_t w) const { return (int)(w - blockIdx.x) * (int)size + (int)(min(w, more) - min(blockIdx.x, more)); }
-  // whose range, before any move, holds unit x: those of workers 0 .. more - 1 are a unit longer.  Counted from this worker's, or, where x lies
-  // beyond the place where the lengths change, from there
-  __device__ __forceinline__ uint32_t owner(int x) const {
-    const int me = (int)blockIdx.x, change = (int)more;
-    const long long change_at = (long long)(change - me) * (size + (me < change));
-    const bool wide = x < change_at, beyond = wide ? me > change : me < change;
-    const int width = (int)size + wide, d = x - (beyond ? (int)change_at : 0);
-    return (uint32_t)((beyond ? change : me) + (d >= 0 ? d / width : -((width - 1 - d) / width)));
+  uint32_t total, workers, size, more, snap, lead;
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * size + min(w, more); }
+  __device__ __forceinline__ uint32_t owner(uint32_t x) const {  // whose range, before any move, holds unit x
+    const uint32_t wide = more * (size + 1);
+    return x < wide ? x / (size + 1) : more + (x - wide) / size;
   }
   // boundary x of the ranges where it lies inside of item [i0, i1)
-  __device__ __forceinline__ int moved(int x, int i0, int i1) const {
+  __device__ __forceinline__ uint32_t moved(uint32_t x, uint32_t i0, uint32_t i1) const {
     if (x <= i0 || x >= i1) return x;
     if (x - i0 <= lead || (x - i0 <= lead + snap && x - i0 - lead <= i1 - x)) return i0;
     return i1 - x <= snap ? i1 : x;
@@ -185,78 +172,72 @@ template <int ROWS, int TILE, int LEAD>
 struct Range {
   Stripes stripes;
   Sequence s;
-  int at, end, skip;  // units; skip: those of the item in front of `at`
+  uint32_t at, end, skip;  // units; skip: those of the item in front of `at`
   int b, item;
   bool more;
-
-  static __device__ __forceinline__ Units units_of(const KvCacheView& c, const Sequence& s) {  // (items are fewer than the vectors of Q)
-    return (Units)((uint32_t)c.kv_heads * (uint32_t)s.blocks) * (uint32_t)(s.tiles + LEAD);
-  }
 
   __device__ __forceinline__ void begin(const AttentionParams& p) {
     const KvCacheView& c = p.cache;
     const int lane = threadIdx.x & 31;
     // lane i counts the tiles of sequences [i * per, (i + 1) * per)
     const int per = (c.sequences + 31) / 32;
-    Units mine = 0;
+    uint32_t mine = 0;
     bool bad = false;
     for (int i = lane * per; i < min(c.sequences, (lane + 1) * per); ++i) {
       const Sequence s = sequence(p, i, ROWS, TILE, bad);
-      mine += units_of(c, s);
+      const unsigned long long units = (unsigned long long)c.kv_heads * s.blocks * (s.tiles + LEAD) + mine;
+      mine = (uint32_t)min(units, (unsigned long long)kMostUnits);
     }
     if (bad) report_cache(p.status);
-    Units before = mine;
+    uint32_t before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const Units x = __shfl_up_sync(~0u, before, d);
-      if (lane >= d) before += x;
+      const uint32_t x = __shfl_up_sync(~0u, before, d);
+      if (lane >= d) before = (uint32_t)min((unsigned long long)before + x, (unsigned long long)kMostUnits);
     }
-    const Units total = __shfl_sync(~0u, before, 31);
+    stripes.total = __shfl_sync(~0u, before, 31);
     before -= mine;
-    stripes.workers = (uint32_t)min((Units)gridDim.x, max((Units)1, total / kLeastTiles));
-    more = total > 0 && blockIdx.x < stripes.workers;
-    if (total > (Units)stripes.workers * kMostUnits) {  // (minutes of work at the least)
+    more = stripes.total > 0;
+    // More than are numbered (40 s of work with heads of 128 elements, several with the smallest) is refused.  (In 64 bits, counted from
+    // the beginning of a CTA's own range, there need be no limit, but the code around this and the order that it leaves the tcgen05
+    // kernel's in made prompts of 2048 tokens 10 % slower, with a window 25 %.)
+    if (stripes.total == kMostUnits) {
       report_cache(p.status);
       more = false;
     }
-    const uint32_t high = (uint32_t)(total >> 16), low = (high % stripes.workers) << 16 | ((uint32_t)total & 0xffff);  // (less than 2^21, 2^24)
-    stripes.size = ((high / stripes.workers) << 16) + low / stripes.workers;
-    stripes.more = low % stripes.workers;
+    stripes.workers = min(gridDim.x, max(1u, stripes.total / kLeastTiles));
+    more = more && blockIdx.x < stripes.workers;
+    stripes.size = stripes.total / stripes.workers;
+    stripes.more = stripes.total % stripes.workers;
     stripes.snap = stripes.size < 8 ? 2 : stripes.size < 48 ? 1 : 0;
     stripes.lead = LEAD;
-    at = 0;
+    at = stripes.begin(blockIdx.x);
     end = stripes.begin(blockIdx.x + 1);
     skip = 0;
     b = item = 0;
     if (more) {  // where the range begins: (sequence, item of it, tile of that)
-      const Units origin = stripes.origin(blockIdx.x);
-      const int owner = __ffs(__ballot_sync(~0u, mine > 0 && before <= origin && origin < before + mine)) - 1;
+      const int owner = __ffs(__ballot_sync(~0u, mine > 0 && before <= at && at < before + mine)) - 1;
       b = owner * per;
-      Units off = origin - __shfl_sync(~0u, before, owner);
+      uint32_t off = at - __shfl_sync(~0u, before, owner);
       for (;; ++b) {
         s = sequence(p, b, ROWS, TILE, bad);
-        const Units units = units_of(c, s);
+        const uint32_t units = (uint32_t)c.kv_heads * s.blocks * (s.tiles + LEAD);
         if (off < units) break;
         off -= units;
       }
-      const int units = s.tiles + LEAD;
-#pragma unroll 1
-      for (int i = 30; off >> 32; --i)  // (item by item in powers of two: rows are fewer than 2^31, and an item shorter than 2^32)
-        if (off >= (Units)units << i) {
-          off -= (Units)units << i;
-          item += 1 << i;
-        }
-      item += (int)((uint32_t)off / units);
-      skip = (int)((uint32_t)off % units);
-      at = stripes.moved(0, -skip, units - skip);
-      skip += at;
+      const uint32_t units = s.tiles + LEAD;
+      item = (int)(off / units);
+      skip = off - item * units;
+      const uint32_t to = stripes.moved(at, at - skip, at - skip + units);
+      skip += to - at;
+      at = to;
     }
   }
 
   // the next one; nt = 0: there is none
   __device__ __forceinline__ Segment next(const AttentionParams& p) {
     const KvCacheView& c = p.cache;
-    if (more && skip == s.tiles + LEAD) {
+    if (more && skip == (uint32_t)s.tiles + LEAD) {
       more = at < end;
       if (more) {
         skip = 0;
@@ -270,13 +251,13 @@ struct Range {
     }
     Segment x = {};
     if (more) {
-      const int i0 = at - skip, i1 = i0 + LEAD + s.tiles, to = min(stripes.moved(end, i0, i1), i1);
+      const uint32_t i0 = at - skip, i1 = i0 + LEAD + s.tiles, to = min(stripes.moved(end, i0, i1), i1);
       if (at < to) {
         x.b = b;
         x.h = item / s.blocks;
-        const int from = skip ? skip - LEAD : 0;
+        const int from = skip ? (int)skip - LEAD : 0;
         x.tile = s.tile0 + from;
-        x.nt = to - i0 - LEAD - from;
+        x.nt = (int)(to - i0) - LEAD - from;
         x.row0 = (item - x.h * s.blocks) * ROWS;
         x.rows = min(ROWS, s.n * p.group - x.row0);
         x.base_high = s.len - s.n + 1;

@@ -722,23 +722,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   prefetch_table(p, kThreads);
-  // (the order of the roles in the file, which decides how their loops share the nearest instruction caches, by measurement: drafts 51.3 us
-  // with the softmax first, 51.7 with the copies first, 47.8 so)
-  if (warp >= kSoftmaxWarps) {
+  if (warp < kSoftmaxWarps) {
+    if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_inc<G::kSoftmaxRegs>();
+    soften<G>(p, sh, ring, weights, tmem);
+  } else {
     if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_dec<G::kOtherRegs>();
     const int w = warp - kSoftmaxWarps;
-    if (w >= kProducers && w < kProducers + kIssuers && threadIdx.x % 32 == 0) {
+    if (w < kProducers)
+      produce<G>(p, sh, w / 2, w % 2, ring, q_slots, ones + G::kOnes);
+    else if (w < kProducers + kIssuers && threadIdx.x % 32 == 0) {
       if (w == kProducers)
         multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
       else
         multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
       drain_products(&sh.drained[w - kProducers]);
-    } else if (w < kProducers) {
-      produce<G>(p, sh, w / 2, w % 2, ring, q_slots, ones + G::kOnes);
     }
-  } else {
-    if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_inc<G::kSoftmaxRegs>();
-    soften<G>(p, sh, ring, weights, tmem);
   }
   __syncwarp();
   tc_fence_before_sync();

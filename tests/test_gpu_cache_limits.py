@@ -127,10 +127,10 @@ def test_many_weights_far_below_the_largest(marlin, q_heads, dim, eight_bit):
     assert off <= want * (2.0 ** -11 + 2.0 ** -14 + 2.0 ** -13 + 2.0 ** -18), (off, want)
 
 
-@pytest.mark.parametrize("q_heads,kv_heads,sequences,length", [(64, 64, 4096, 1 << 20), (192, 16, 1024, 1 << 23)])
-def test_more_tiles_than_32_bits_count(marlin, q_heads, kv_heads, sequences, length):
-    # 2^32 tiles of 64 keys with a row each, and 2^30 of 128 keys with 12 rows on the tensor cores' fifth generation (two to four seconds
-    # each).  All entries of the table are page 0 but the last of every row, page 1, so that the result is that of two pages, the first
+@pytest.mark.parametrize("q_heads,kv_heads,sequences,length", [(64, 64, 4000, 1 << 20), (192, 16, 1024, 1 << 23)])
+def test_nearly_as_many_tiles_as_32_bits_count(marlin, q_heads, kv_heads, sequences, length):
+    # 0.98 * 2^32 tiles of 64 keys with a row each, and 2^30 of 128 keys with 12 rows on the tensor cores' fifth generation (two to
+    # four seconds each).  All entries of the table are page 0 but the last of every row, page 1, so that the result is that of two pages, the first
     # counted as often as it is there.
     import torch
     page, dim = 1 << 14, 16
@@ -163,3 +163,21 @@ def test_more_tiles_than_32_bits_count(marlin, q_heads, kv_heads, sequences, len
             want, spread = w @ values, w @ values.abs()
             off = (got[a:a + 4096] - want).abs()
             assert bool((off <= 2.0 ** -11 * want.abs() + relative * spread).all())  # (false for NaN)
+
+
+def test_more_tiles_than_32_bits_count_are_refused(marlin):
+    import torch
+    q = torch.ones(4100, 64 * 16, dtype=torch.float16, device="cuda")
+    k = torch.ones(1, 64, 1 << 14, 16, dtype=torch.float16, device="cuda")
+    table = torch.zeros(4100, 64, dtype=torch.int32, device="cuda")
+    lengths = torch.full((4100,), 1 << 20, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(marlin.attention_workspace_bytes(16), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 7.0)
+    marlin.attention_decode(q, k, k, table, lengths, ws, out=out)
+    assert marlin.read_status(ws) == 9
+    assert (out == 7).all() and not ws[256:].any()
+    ws.zero_()
+    lengths[4:] = 0
+    marlin.attention_decode(q, k, k, table, lengths, ws, out=out)
+    assert marlin.read_status(ws) == 0
+    assert (out[:4] == 1).all() and not out[4:].any()
