@@ -21,7 +21,8 @@
 // costs its thread some 75 cycles and a commit 125, and with one thread for all of them everybody waited for it.
 // An 8-bit cache (of 128 elements, for more than 32 rows) is converted to fp16 by the warps that copy: the products take operands of
 // one type, and fp16 is what Q and the weights have.  The conversion bounds that: some 260 cycles for 16 keys of one warp.
-// Keys and values have rings of their own: values are held until the weights of their keys are there, and keys need not wait for that.  Tensor memory: S twice, and O; N columns each.
+// Keys and values have rings of their own: values are held until the weights of their keys are there, and keys need not wait for that.
+// Tensor memory: S twice, O, and what of O was put aside (kFold); N columns each.
 #include "attention.cuh"
 #include "tc_utils.cuh"
 
@@ -30,6 +31,11 @@ namespace {
 
 constexpr int kTile = 128;
 constexpr int kLead = 4;                 // what an item costs beside its tiles, in tiles
+// Tiles whose results are summed in the products.  A product adds to its sums in fp32 but cuts off what lies below them, key by key, so that
+// sums over 131 thousand keys come out too small by 2^-10.5 (7e-4, measured; over 524 thousand by 2.8e-3, where the weights are summed
+// elsewhere), more than half a step of fp16.  After so many tiles they are therefore added to others, rounded, and
+// begin again: 1e-4 whatever the length.  That is one pause in 16384 keys.
+constexpr int kFold = 128;
 constexpr int kBlock = kTile * 128;      // 64 elements of the keys of a tile: rows of 128 bytes, as the swizzle has them
 constexpr int kSoftmaxWarps = 8;
 constexpr int kSoftmaxThreads = kSoftmaxWarps * 32;
@@ -65,7 +71,7 @@ struct TcGeometry {
   static constexpr int kSoftmaxRegs = N == 64 ? 160 : 0, kOtherRegs = 96;
   static_assert(8 * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "registers");
   static constexpr int kSmem = kSlots * kSlot + kRest + kProducers * kRaw * kRawBytes + 1024;  // (the ring begins at a multiple of 1024)
-  static constexpr int kColumns = 4 * N;           // of tensor memory: S, S, O, and N that a power of two brings along
+  static constexpr int kColumns = 4 * N;           // of tensor memory: S, S, O, and O put aside
   static constexpr int kMine = N / 2;              // rows of a half of the softmax warps
   static_assert(kKeySlots >= 2 && kColumns <= 512, "ring");
 };
@@ -393,7 +399,7 @@ __device__ __forceinline__ void multiply(const AttentionParams& p, TcShared<G>& 
         for (int ks = 0; ks < kTile / 16; ++ks) {
           const uint32_t v = values + ks * 2048;
           mma_ss(tmem + 2 * N, desc_columns(v, G::kSumRows ? ones - v : kBlock), desc_weights<G::kPRow>(w + ks * 16 * G::kPRow),
-                 kColumnsDesc, i || ks ? 1 : 0);
+                 kColumnsDesc, i % kFold || ks ? 1 : 0);
         }
         tc_commit(&sh.p_done[pb]);
         tc_commit(&sh.empty[slot]);
@@ -508,7 +514,8 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         y[r + 3] = fmaf(y[r + 3], factor, -base.w);
         top = fmaxf(fmaxf(fmaxf(top, y[r]), fmaxf(y[r + 1], y[r + 2])), y[r + 3]);
       }
-      const bool over = fresh || top > kSlack;
+      const bool unseen = pos0 + kTile <= sees.low_min || pos0 >= sees.high_max;  // by any row: weights of 0, whatever the bases are
+      const bool fold = i % kFold == 0 && i > 0, over = (fresh && !unseen) || fold || top > kSlack;
       if (any_of(1 + half, 128, over)) {  // move the bases: the largest logit of every row over the 128 keys
 #pragma unroll
         for (int r = 0; r < kMine; ++r) {
@@ -546,6 +553,14 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
 #pragma unroll
             for (int r = 0; r < 8; ++r) z[r] *= sh.alpha[mine + r0 + r];
             store_columns(lanes + 2 * N + mine + r0, z);
+            if (i >= kFold) {  // those that were put aside, and these to them
+              float aside[8];
+              load_columns(lanes + 3 * N + mine + r0, aside);
+              tc_wait_ld();
+#pragma unroll
+              for (int r = 0; r < 8; ++r) aside[r] = (i > kFold ? aside[r] * sh.alpha[mine + r0 + r] : 0.f) + (fold ? z[r] : 0.f);
+              store_columns(lanes + 3 * N + mine + r0, aside);
+            }
           }
           tc_wait_st();
         }
@@ -606,6 +621,19 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
     const uint32_t last = u - 1;
     wait(&sh.p_done[last % G::kPBuffers], last / G::kPBuffers & 1);
     tc_fence_after_sync();
+    if (nt > kFold) {  // what was put aside joins the rest
+#pragma unroll 1
+      for (int r0 = 0; r0 < kMine; r0 += 8) {
+        float z[8], aside[8];
+        load_columns(lanes + 2 * N + mine + r0, z);
+        load_columns(lanes + 3 * N + mine + r0, aside);
+        tc_wait_ld();
+#pragma unroll
+        for (int r = 0; r < 8; ++r) z[r] += aside[r];
+        store_columns(lanes + 2 * N + mine + r0, z);
+      }
+      tc_wait_st();
+    }
     if (G::kSumRows && (warp & 3) == 2) {  // (lanes 64 - 127 all have them)
       float z[kMine];
       load_columns(lanes + 2 * N + mine, z);
@@ -722,20 +750,22 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const Attenti
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   prefetch_table(p, kThreads);
+  // (the order of the roles in the file decides how their loops share the nearest instruction caches, and is the best of three: with the
+  // copies in front of the products prompts of 2048 tokens take 3 % longer, with the softmax last drafts 1 % and windows 3 %)
   if (warp < kSoftmaxWarps) {
     if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_inc<G::kSoftmaxRegs>();
     soften<G>(p, sh, ring, weights, tmem);
   } else {
     if constexpr (G::kSoftmaxRegs > 0) setmaxnreg_dec<G::kOtherRegs>();
     const int w = warp - kSoftmaxWarps;
-    if (w < kProducers)
-      produce<G>(p, sh, w / 2, w % 2, ring, q_slots, ones + G::kOnes);
-    else if (w < kProducers + kIssuers && threadIdx.x % 32 == 0) {
+    if (w >= kProducers && w < kProducers + kIssuers && threadIdx.x % 32 == 0) {
       if (w == kProducers)
         multiply<G, kLogits>(p, sh, ring, q_slots, weights, ones, tmem);
       else
         multiply<G, kResults>(p, sh, ring, q_slots, weights, ones, tmem);
       drain_products(&sh.drained[w - kProducers]);
+    } else if (w < kProducers) {
+      produce<G>(p, sh, w / 2, w % 2, ring, q_slots, ones + G::kOnes);
     }
   }
   __syncwarp();

@@ -181,3 +181,37 @@ def test_more_tiles_than_32_bits_count_are_refused(marlin):
     marlin.attention_decode(q, k, k, table, lengths, ws, out=out)
     assert marlin.read_status(ws) == 0
     assert (out[:4] == 1).all() and not out[4:].any()
+
+
+@pytest.mark.parametrize("q_heads,dim,eight_bit", [(12, 128, False), (20, 112, False), (40, 128, False), (16, 64, False), (64, 64, False),
+                                                   (40, 128, True), (64, 80, True)])
+@pytest.mark.parametrize("rising", [False, True])
+@pytest.mark.parametrize("n", [16384, 16385, 33000, 524299])
+def test_sums_over_long_ranges_of_keys(marlin, q_heads, dim, eight_bit, rising, n):
+    # More items than CTAs, so that some CTAs have all the keys of an item; values around 1, so that what a sum loses shows; logits that rise
+    # with the position, so that bases move after sums were put aside.  Allowed: the result's rounding and that of the weights,
+    # 2^-11 each, and what 16384 keys lose one by one, at most 2^-23 of a sum that grows from 0, 2^-24 of it on the average:
+    # 2^-10.  (Exponentials, factors and the rest are below 2^-16.)
+    import torch
+    page, sequences = 1024, 200 if n > 1 << 17 else 300
+    kind = torch.float8_e4m3fn if eight_bit else torch.float16
+    gen = torch.Generator(device="cuda").manual_seed(n + dim)
+    pages = -(-n // page)
+    k = torch.randn(pages * page, dim, generator=gen, device="cuda")
+    if rising:
+        k[:, 0] = torch.arange(pages * page, device="cuda") * (16.0 / n)
+    k = k.to(kind)
+    v = (torch.rand(pages * page, dim, generator=gen, device="cuda") + 0.5).to(kind)
+    q = (torch.randn(q_heads, dim, generator=gen, device="cuda") * 0.7).half()
+    if rising:
+        q[:, 0] = dim ** 0.5 * 3.0
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(sequences, 1)
+    lengths = torch.full((sequences,), n, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(marlin.attention_workspace_bytes(dim), dtype=torch.uint8, device="cuda")
+    out = marlin.attention_decode(q.repeat(sequences, 1, 1).view(sequences, -1), k.view(pages, 1, page, dim), v.view(pages, 1, page, dim),
+                                  table, lengths, ws)
+    assert marlin.read_status(ws) == 0
+    w = torch.softmax(q.double() @ k[:n].double().T * dim ** -0.5, -1)
+    want = w @ v[:n].double()
+    off = (out.double().view(sequences, q_heads, dim) - want).abs() / want
+    assert bool((off <= 2.0 ** -11 + 2.0 ** -11 + 2.0 ** -10 + 2.0 ** -16).all()), off.max()
