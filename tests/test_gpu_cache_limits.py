@@ -215,3 +215,29 @@ def test_sums_over_long_ranges_of_keys(marlin, q_heads, dim, eight_bit, rising, 
     want = w @ v[:n].double()
     off = (out.double().view(sequences, q_heads, dim) - want).abs() / want
     assert bool((off <= 2.0 ** -11 + 2.0 ** -11 + 2.0 ** -10 + 2.0 ** -16).all()), off.max()
+
+
+@pytest.mark.parametrize("q_heads,dim", [(1, 64), (8, 128), (5, 80), (3, 256), (12, 64), (16, 128), (40, 64), (40, 128), (24, 256)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_infinite_values_that_every_row_sees(marlin, q_heads, dim, new):
+    import torch
+    case = Case([70, 300, 9], new, q_heads, 1, dim, 16, seed=dim + new)
+    d = case.dev(marlin)
+    q = torch.from_numpy(case.q.reshape(case.T, -1)).cuda() * 0.25  # (no weight is below 2^-10 of the largest)
+    want = marlin.attention_decode(q, **d).view(3, new, q_heads, dim).clone()
+    v = d["v_cache"].clone()
+    inf, nan = float("inf"), float("nan")
+
+    def value(b, pos, element, x):
+        v[int(case.table[b][pos // 16]), 0, pos % 16, element] = x
+    # keys in every part of a tile and of the sequence
+    value(0, 3, 1, inf), value(0, 40, 2, -inf), value(0, 5, 3, inf), value(0, 60, 3, inf), value(0, 17, 4, inf), value(0, 18, 4, -inf)
+    value(1, 250, 5, inf), value(1, 1, 6, -inf), value(1, 130, 7, nan), value(2, 0, 8, inf)
+    got = marlin.attention_decode(q, **{**d, "v_cache": v}).view(3, new, q_heads, dim)
+    torch.cuda.synchronize()
+    assert marlin.read_status(d["workspace"]) == 0
+    want[0, :, :, 1], want[0, :, :, 2], want[0, :, :, 3], want[0, :, :, 4] = inf, -inf, inf, nan
+    want[1, :, :, 5], want[1, :, :, 6], want[1, :, :, 7], want[2, :, :, 8] = inf, -inf, nan, inf
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    fine = ~torch.isnan(want)
+    assert torch.equal(got[fine], want[fine])
