@@ -29,8 +29,8 @@ def rotate(x, position, inv_freq, interleaved):
 
 
 def attention(q, k_cache, v_cache, table, lengths, starts, scale, window=0, k_scale=None, v_scale=None):
-    """q [T, q_heads, head_dim] -> (out, spread, logit_error, keys), float64.  `spread` is sum_j w_j |v_j|, `small` sum_j |v_j|,
-    and `mass` the largest sum_d |q_d k_d| * scale of a row: what bounds on rounding errors are made of."""
+    """q [T, q_heads, head_dim] -> (out, spread, small, mass, keys), float64.  `spread` is sum_j w_j |v_j|, `small` sum_j |v_j|,
+    `mass` the largest sum_d |q_d k_d| * scale of a row, `keys` how many it sees: what bounds on rounding errors are made of."""
     T, Hq, D = q.shape
     Hkv, P = k_cache.shape[1], k_cache.shape[2]
     out = np.zeros((T, Hq, D))

@@ -15,11 +15,12 @@
 // The products are mma.sync.m16n8k16 with the keys (of S^T = K Q^T) and the values (of O^T = V^T P^T) on the 16-wide side and
 // the rows on the 8-wide one: a decode step has few rows, and eight of them fill an operand.
 //
-// Measured, back to back in a graph: 64 sequences of 2000 to 4096 keys, 32 heads of 128 elements, 456 us, 7.0 TB/s; 64 of up to 8191 keys that
+// Measured, back to back in a graph: 64 sequences of 2000 to 4096 keys, 32 heads of 128 elements, 458 us, 7.0 TB/s; 64 of up to 8191 keys that
 // eight query heads share, 160 us, 6.7 TB/s; one of 131009 keys, 88 us, 6.1 TB/s; 16 of 500 to 1531 keys, 47 us, 5.8 TB/s: a call costs some
-// 8.5 us beside the time of its bytes, of which 4 pass before the first products (launch, ranges, page numbers, first keys) and 4 in
-// CTAs that end before others and in the joining of parts; one of 129 keys takes 5.9.  8-bit caches, 32 of 2000 to 4099 keys: 44 us,
-// 4.6 TB/s, where the copies alone take 38: every element is converted by the warp that multiplies it.
+// 8.4 us beside the time of its bytes, of which 4 pass before the first products (launch, ranges, page numbers, first keys) and 4 in
+// CTAs that end before others and in the joining of parts; one of 129 keys takes 5.8.  8-bit caches, 32 of 2000 to 4099 keys, 64 heads
+// over 8: 43 us, 4.7 TB/s, where the copies alone take 38.  No unit is full there (issue 36 %, ALU 32 %, tensor 13 %, DRAM 54 %): two warps
+// that multiply on each scheduler wait for what they convert and for what that is multiplied with.
 #include "attention.cuh"
 
 namespace marlin_b200 {
@@ -582,11 +583,13 @@ cudaError_t launch(const AttentionParams& p, int sm_count, cudaStream_t stream) 
 }
 template <int DP, bool F8>
 cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t stream) {
+  // (Both sides of each choice at one size: 16 sequences of 1000 to 4099 keys, eight heads of keys.  With sequences of a few dozen keys an
+  // item of one tile costs far more on tcgen05 than its bytes, 57 us for 121 of them with 8 or 16 rows against a floor of 3, and
+  // nothing here looks at how long they can be.)
   // Up to eight rows: a warp has them all beside the keys.  More of them, over fp16: the tensor cores' fifth generation (16 rows of 128
   // elements: 39.3 us there, 39.9 here; 32 rows: 43 and 47; 48 rows: 47 and 53).  More of them over 8 bits: here, where
   // every warp converts what it multiplies (16 rows: 31 us here, 46 there; 32 rows: 45 and 49), until the products are what takes
-  // the time, with more than 32 rows of 128 elements (48 rows: 72 and 55; of 64 elements: 44 and 46).  16 sequences of 1000 to
-  // 4099 keys, eight heads of keys.  A warp holds 8 NT rows of sums (DP * NT / 4 registers a thread); more rows than that
+  // the time, with more than 32 rows of 128 elements (48 rows: 72 and 55; of 64 elements: 44 and 46).  A warp holds 8 NT rows of sums (DP * NT / 4 registers a thread); more rows than that
   // share keys and values between the warps of a team.
   const long long rows = usual_rows(p);
   if (rows <= 8) return launch<DP, 1, 1, F8>(p, sm_count, stream);

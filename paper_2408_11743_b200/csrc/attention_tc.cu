@@ -11,8 +11,9 @@
 // What bounds it: the products read every key and value from shared memory once, 128 bytes a cycle: 512 cycles for a tile of
 // 64 KB, which takes 2800 to come from memory.  (A third product, of ones with the weights, cost as much as either of the two.)
 // So the memory should bound it, and does not: 16 sequences of 1000 to 4099 keys with 48 rows for each of eight heads of 128 elements take
-// 47.5 us (3.7 TB/s; the copies alone 40.6, mma.sync in its place 53), 24 of 900 to 16001 keys seen through a window of 2048, 29 rows of 64
-// elements, 35 us (2.8 TB/s; copies alone 28, mma.sync 36).  What they wait for: the chain of one tile, from its logits through the
+// 47.6 us (3.7 TB/s; the copies alone 40.6, mma.sync in its place 53), 24 of 900 to 16001 keys seen through a window of 2048, 29 rows of 64
+// elements, 35 us (2.8 TB/s; copies alone 28, mma.sync 36).  So most of the distance to the time of their bytes, 26.6 and 14.9 us, lies in
+// the copies and in what a call costs beside them (17 and 15 us).  The rest: the chain of one tile, from its logits through the
 // weights to the second product, where an item has few tiles; the ends of the items; and instructions, since softmax, moves of
 // the bases, read-out and joining do not fit into the nearest caches together (their order in the file moves these times by a tenth).
 //

@@ -9,7 +9,7 @@
 // What bounds it: the bytes where there are many tokens (10800 of them with 32 heads each of queries, keys and values: 82 us, 6.5 TB/s, of
 // reads and writes in equal parts, as fast as a copy; 97 us with divisions by run-time numbers in place of multiplications and with
 // sines that lay in the order of the pairs, four lanes to a bank: 62 % of the issue slots were taken), and one chain of dependent
-// loads (length, page number, then the stores) where there are few: 2.2 us for one token, 2.8 for 64.
+// loads (length, page number, then the stores) where there are few: 2.2 us for one token, 2.9 for 64.
 #include "kv_cache.cuh"
 
 namespace marlin_b200 {
@@ -196,7 +196,7 @@ cudaError_t launch_kv_append(AppendParams p, int tokens, int interleaved, int sm
   p.head_magic = magic_of(p.head_units);
   p.value_magic = magic_of(p.cache.head_dim / 8);
   p.units = (p.q_heads + p.cache.kv_heads) * p.head_units + p.cache.kv_heads * (p.cache.head_dim / 8);
-  // a few tokens: their heads are spread over more CTAs, until the SMs have one each
+  // a few tokens: their heads are spread over more CTAs, until the SMs have two each
   p.units_per_thread = kMostUnits;
   while (p.units_per_thread > 1 &&
          (long long)tokens * ((p.units + kThreads * p.units_per_thread - 1) / (kThreads * p.units_per_thread)) < 2 * sm_count)

@@ -162,7 +162,8 @@ struct AttentionParams {
 };
 size_t attention_slot_bytes(int head_dim);
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream);
-// where a key head of an fp16 cache has more than eight rows (attention_tc.cu); head_dim up to 128
+// head_dim up to 128, where a key head has more than eight rows of an fp16 cache, or more than 32 of 128 elements of an 8-bit one
+// (launch_rows in attention.cu; the kernel is in attention_tc.cu)
 cudaError_t launch_attention_tc(const AttentionParams& p, int sm_count, cudaStream_t stream);
 
 // ---- the stripe partition (host and device use the same two formulas) ------------------------
