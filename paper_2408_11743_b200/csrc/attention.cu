@@ -589,8 +589,8 @@ cudaError_t launch_rows(const AttentionParams& p, int sm_count, cudaStream_t str
   // Up to eight rows: a warp has them all beside the keys.  More of them, over fp16: the tensor cores' fifth generation (16 rows of 128
   // elements: 39.3 us there, 39.9 here; 32 rows: 43 and 47; 48 rows: 47 and 53).  More of them over 8 bits: here, where
   // every warp converts what it multiplies (16 rows: 31 us here, 46 there; 32 rows: 45 and 49), until the products are what takes
-  // the time, with more than 32 rows of 128 elements (48 rows: 72 and 55; of 64 elements: 44 and 46).  A warp holds 8 NT rows of sums (DP * NT / 4 registers a thread); more rows than that
-  // share keys and values between the warps of a team.
+  // the time, with more than 32 rows of 128 elements (48 rows: 72 and 55; of 64 elements: 44 and 46).  A warp holds 8 NT rows of
+  // sums (DP * NT / 4 registers a thread); more rows than that share keys and values between the warps of a team.
   const long long rows = usual_rows(p);
   if (rows <= 8) return launch<DP, 1, 1, F8>(p, sm_count, stream);
   if (DP < 256 && (!F8 || (DP == 128 && rows > 32))) return launch_attention_tc(p, sm_count, stream);
