@@ -348,6 +348,88 @@ MARLIN_API int marlin_attention_block(const void* A, const void* w_qkv, const vo
                            int interleaved, float scale, int window,
                            void* workspace, size_t workspace_bytes, marlin_stream stream);
 
+/* ---- the same cache in 8 bits with a scale for each block of tokens, and with first tokens that stay visible -------- */
+
+#define MARLIN_KV_INT8 2  /* `format` of a cache of the calls below that is given scales by block: codes in two's complement */
+
+/* Scales of an 8-bit cache (MARLIN_KV_E4M3 or MARLIN_KV_INT8; its own k_scale and v_scale are NULL then): a code of head h of the token
+ * at position p stands for its value times
+ *   k[page * stride[0] + h * stride[1] + (p % page_size) / block_size * stride[2]]       (page: its page of the table; v alike)
+ * Strides count floats.  block_size is a power of two, at most page_size and 128.  No two scales share a place. */
+typedef struct {
+  float* k;           /* device */
+  float* v;           /* device */
+  int64_t stride[3];  /* floats between pages, heads and blocks */
+  int block_size;     /* tokens */
+} marlin_kv_scales;
+
+/* marlin_kv_append into such a cache, whose scales are made on the way: nothing has to be measured beforehand.  With L the largest code (127;
+ * 448 in e4m3) and a the largest magnitude of the new elements of a head in a block, after the rotation, that is finite:
+ *   a block whose first token is among the new ones gets the scale s = a / L, whatever it held before;
+ *   one that has tokens already keeps its scale if a / L <= s, otherwise s is doubled until that is so, and the codes of its earlier tokens
+ *   are divided by the same power of two and rounded to nearest even (so a code loses at most a step of the block's last scale, however often
+ *   that grew; nothing in e4m3 except where it becomes subnormal).  A scale that is not finite and above 0 stands for codes of 0.
+ *   codes are the nearest (even) of x * (1 / s) in fp32; an infinity becomes the largest code, a NaN stays one in e4m3 and is 0 in two's
+ *   complement; all codes are 0 where a is 0.
+ * Everything else as marlin_kv_append.  The same inputs give the same bits on every call; a prompt in two calls can give other ones than in one. */
+MARLIN_API int marlin_kv_append_scaled(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            void* q_out, const marlin_kv_cache* cache, const marlin_kv_scales* scales, const int32_t* starts, int tokens,
+                            int q_heads, const float* inv_freq, int rotary_dim, int interleaved,
+                            void* workspace, size_t workspace_bytes, marlin_stream stream);
+
+/* marlin_attention_decode over any cache of this header (scales NULL: fp16, or e4m3 with scales by key head), where a token at position p sees
+ * besides the `window` last positions the first `sinks` ones: j <= p and (j > p - window or j < sinks).  (sinks mean nothing without
+ * a window.)  Results, errors and limits as there, with three differences:
+ *   with scales by block the weights are rounded to fp16 together with the scales of their values, so a product w_j s_j is off by at most
+ *   2^-11 of it, or 2^-31 of the largest weight of its row times the largest scale that it meets, if that is more;
+ *   blocks of rows go only over tiles that some of their rows can see, so that a prompt with a window costs what the window holds;
+ *   a scale that is not finite reaches the rows that see its tokens, and no others. */
+MARLIN_API int marlin_attention_sinks(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const marlin_kv_scales* scales,
+                           const int32_t* starts, int tokens, int q_heads, float scale, int window, int sinks, void* out,
+                           void* workspace, size_t workspace_bytes, marlin_stream stream);
+
+/* marlin_attention_block with marlin_kv_append_scaled (where scales are given) and marlin_attention_sinks in the middle. */
+MARLIN_API int marlin_attention_block_sinks(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o,
+                                 void* QKV, void* Q, void* O, void* C, const marlin_kv_cache* cache, const marlin_kv_scales* scales,
+                                 const int32_t* starts, int M, int K, int q_heads, int N, int group_size, const float* inv_freq,
+                                 int rotary_dim, int interleaved, float scale, int window, int sinks,
+                                 void* workspace, size_t workspace_bytes, marlin_stream stream);
+
+/* ---- page tables from lengths ------------------------------------------------------------------------------------- */
+
+/* The pages of a cache as marlin_kv_reserve keeps them (a host structure of device pointers; what they point to is read and written). */
+typedef struct {
+  int32_t* table;       /* device, [sequences][max_pages]: page numbers of each sequence, as in marlin_kv_cache */
+  int64_t table_stride;
+  int32_t* lengths;     /* device, [sequences]: tokens of each sequence */
+  int32_t* free_pages;  /* device, [capacity]: numbers of pages that nobody has; the last of the first free_count[0] is handed out first */
+  int32_t* free_count;  /* device, [1] */
+  int capacity;         /* of free_pages: as many as there are pages */
+  int max_pages;
+  int sequences;
+  int page_size;        /* tokens, a power of two */
+} marlin_kv_pages;
+
+/* Makes room for the new tokens of a step, and takes back what sequences do not need any more.  Sequence b with lengths[b] tokens keeps the first
+ * min(keep[b], lengths[b]) of them and gets counts[b] new ones behind these; lengths[b] becomes the sum.  (Drafted tokens that were not
+ * accepted: keep is less than the length.  A sequence that ends: keep and count 0.)
+ *   counts     device, int32 [sequences], or NULL: one each;   keep   device, int32 [sequences], or NULL: all
+ *   tokens     rows of the step: at least the sum of the counts (0: none)
+ *   starts     device, out, int32 [sequences + 1], or NULL: starts[b] = counts[0] + .. + counts[b - 1] (2^31 - 1 if that is less; negative
+ *              counts are none), what the calls above take
+ *   slots      device, out, int64 [tokens], or NULL: table[b][p / page_size] * page_size + p % page_size for the token at position p
+ *   positions  device, out, int32 [tokens], or NULL: p.  Both are -1 in rows behind the last token and in those of refused sequences.
+ * Pages are taken from the top of the stack, in the order of the sequences and of their positions; entries of the table behind the
+ * last page are not touched.  Pages that are not needed any more go back on the stack in the order in which the same pages
+ * would be taken again: a step that is taken back leaves stack and lengths as they were.  They are handed out from the next call on.
+ * A sequence is refused, and left as it was, when fewer pages are free than it and the sequences in front of it need (sequences that need
+ * none are served all the same), when its row of the table is too short, its count negative or its rows lie behind `tokens`.  Its length
+ * becomes -1 - length: the calls above leave it out and report it, and the next call here takes it for the length again.  (Only the
+ * last three reasons set the status word to MARLIN_ERR_CACHE.)
+ * workspace: at least 8192 bytes under the contract of marlin_workspace_bytes.  One launch; nothing is read on the host. */
+MARLIN_API int marlin_kv_reserve(const marlin_kv_pages* pages, const int32_t* counts, const int32_t* keep, int tokens, int32_t* starts,
+                      int64_t* slots, int32_t* positions, void* workspace, size_t workspace_bytes, marlin_stream stream);
+
 /* Synchronises `stream`, then returns the device-side status word of `workspace`
  * (MARLIN_OK, MARLIN_ERR_DEVICE_TIMEOUT if a kernel gave up a bounded wait, or MARLIN_ERR_CACHE), or
  * MARLIN_ERR_CUDA if the stream reports an error.  The status word is sticky until the

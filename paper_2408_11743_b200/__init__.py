@@ -6,6 +6,8 @@ call loads the library and raises if it is missing (there is no CPU or eager fal
 """
 from .binding import (  # noqa: F401
     KvCache,
+    KvPages,
+    KvScales,
     Layer,
     MarlinError,
     attention_block,
@@ -18,6 +20,7 @@ from .binding import (  # noqa: F401
     gemm_w8,
     interleave_gate_up,
     kv_append,
+    kv_reserve,
     gemm_zp,
     lib,
     mlp_swiglu,

@@ -22,6 +22,7 @@ EXPORTS = [
     "marlin_interleave_gate_up", "marlin_gemm_swiglu", "marlin_mlp_swiglu",
     "marlin_packed_weight_bytes_w8", "marlin_pack_w8", "marlin_unpack_w8", "marlin_gemm_w8",
     "marlin_attention_workspace_bytes", "marlin_kv_append", "marlin_attention_decode", "marlin_attention_block",
+    "marlin_kv_append_scaled", "marlin_attention_sinks", "marlin_attention_block_sinks", "marlin_kv_reserve",
 ]
 STATIC_WS_MAX_M = 16  # MARLIN_STATIC_WS_MAX_M of the header
 
@@ -84,9 +85,13 @@ def lib():
     L.marlin_kv_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i, i, vp, i, i, vp, sz, vp]
     L.marlin_attention_decode.argtypes = [vp, i64, vp, vp, i, i, f32, i, vp, vp, sz, vp]
     L.marlin_attention_block.argtypes = [vp] * 11 + [i] * 5 + [vp, i, i, f32, i, vp, sz, vp]
+    L.marlin_kv_append_scaled.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i, i, vp, i, i, vp, sz, vp]
+    L.marlin_attention_sinks.argtypes = [vp, i64, vp, vp, vp, i, i, f32, i, i, vp, vp, sz, vp]
+    L.marlin_attention_block_sinks.argtypes = [vp] * 12 + [i] * 5 + [vp, i, i, f32, i, i, vp, sz, vp]
+    L.marlin_kv_reserve.argtypes = [vp, vp, vp, i, vp, vp, vp, vp, sz, vp]
     L.marlin_read_status.argtypes = [vp, vp]
     L.marlin_plan_stripes.argtypes = [i, i, i, i, vp, vp, vp, i]
-    for name in ("marlin_kv_append", "marlin_attention_decode", "marlin_attention_block", "marlin_pack_w8", "marlin_unpack_w8", "marlin_gemm_w8", "marlin_interleave_gate_up", "marlin_gemm_swiglu", "marlin_mlp_swiglu", "marlin_pack_zeros", "marlin_unpack_zeros", "marlin_gemm_zp", "marlin_quantize_rtn", "marlin_gemm_static_ws", "marlin_pack", "marlin_unpack", "marlin_gemm", "marlin_pack_sparse24", "marlin_unpack_sparse24",
+    for name in ("marlin_kv_append_scaled", "marlin_attention_sinks", "marlin_attention_block_sinks", "marlin_kv_reserve", "marlin_kv_append", "marlin_attention_decode", "marlin_attention_block", "marlin_pack_w8", "marlin_unpack_w8", "marlin_gemm_w8", "marlin_interleave_gate_up", "marlin_gemm_swiglu", "marlin_mlp_swiglu", "marlin_pack_zeros", "marlin_unpack_zeros", "marlin_gemm_zp", "marlin_quantize_rtn", "marlin_gemm_static_ws", "marlin_pack", "marlin_unpack", "marlin_gemm", "marlin_pack_sparse24", "marlin_unpack_sparse24",
                  "marlin_gemm_sparse24", "marlin_read_status", "marlin_plan_stripes"):
         getattr(L, name).restype = i
     _lib = L
@@ -409,6 +414,18 @@ class KvCache(ctypes.Structure):
                 ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int), ("format", ctypes.c_int)]
 
 
+class KvScales(ctypes.Structure):
+    """marlin_kv_scales of the header."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride", ctypes.c_int64 * 3), ("block_size", ctypes.c_int)]
+
+
+class KvPages(ctypes.Structure):
+    """marlin_kv_pages of the header."""
+    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("lengths", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p), ("capacity", ctypes.c_int), ("max_pages", ctypes.c_int), ("sequences", ctypes.c_int),
+                ("page_size", ctypes.c_int)]
+
+
 def attention_workspace_bytes(head_dim: int) -> int:
     n = int(lib().marlin_attention_workspace_bytes(head_dim))
     if n == 0:
@@ -421,38 +438,59 @@ def kv_append(qkv, k_cache, v_cache, pages, lengths, workspace, inv_freq=None, i
     """marlin_kv_append: puts the keys and values of new tokens into a paged cache and rotates queries and keys.
 
     qkv       fp16 [T, (q_heads + 2 kv_heads) * head_dim], as the qkv layer leaves it: queries, keys, values
-    k_cache, v_cache   fp16 or float8_e4m3fn [pages, kv_heads, page_size, head_dim], any strides but the last
+    k_cache, v_cache   fp16, float8_e4m3fn or int8 [pages, kv_heads, page_size, head_dim], any strides but the last
     pages     int32 [B, max_pages]: the pages of each sequence
     lengths   int32 [B]: tokens of each sequence, the new ones included
     workspace uint8, attention_workspace_bytes(head_dim), zeroed once (a layer's workspace serves if it is large enough)
     inv_freq  fp32 [rotary_dim / 2], or None: no rotation;  interleaved: pairs are (2 j, 2 j + 1), not (j, j + rotary_dim / 2)
     starts    int32 [B + 1]: sequence b has the rows starts[b] .. starts[b + 1] - 1; None: one row each
-    k_scale, v_scale   fp32 [kv_heads] of an 8-bit cache, or None: 1
+    k_scale, v_scale   fp32 [kv_heads] of an e4m3 cache, or None: 1.  fp32 [pages, kv_heads, page_size / block] of an int8 or e4m3 cache: a scale
+              for each block of tokens and key head, which the call makes (marlin_kv_append_scaled); any strides but the last, the same for both
 
     Returns the rotated queries [T, q_heads * head_dim]; without inv_freq the columns of qkv that hold them."""
     return native().kv_append(qkv, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, inv_freq,
                               interleaved, out)
 
 
+def kv_reserve(lengths, pages, free_pages, free_count, workspace, page_size: int, tokens: int, counts=None, keep=None, starts=None,
+               slots=None, positions=None, stream=None):
+    """marlin_kv_reserve: makes room for the new tokens of a step in the page tables, and takes back what sequences do not need any more.
+
+    lengths   int32 [B], updated: each sequence keeps min(keep, length) tokens and gets counts new ones; -1 - length where there is no room
+    pages     int32 [B, max_pages], updated: the pages of each sequence
+    free_pages, free_count   int32 [as many as there are pages] and [1], updated: the stack of pages that nobody has
+    workspace uint8, at least 8192 bytes, zeroed once
+    tokens    rows of the step, at least the sum of the counts
+    counts, keep   int32 [B], or None: one new token each; everything is kept
+
+    Returns (starts int32 [B + 1], slots int64 [tokens], positions int32 [tokens]), new ones unless they are given: the first row of each
+    sequence, and of each row its place in the cache (page * page_size + token of the page) and its position, -1 for rows without one."""
+    return native().kv_reserve(lengths, pages, free_pages, free_count, workspace, page_size, tokens, counts, keep, starts, slots, positions,
+                               stream)
+
+
 def attention_decode(q, k_cache, v_cache, pages, lengths, workspace, scale=None, window: int = 0, starts=None, k_scale=None,
-                     v_scale=None, out=None, stream=None):
-    """marlin_attention_decode: attention of new tokens over a paged cache that holds them already (see kv_append).
+                     v_scale=None, out=None, stream=None, sinks: int = 0):
+    """marlin_attention_decode: attention of new tokens over a paged cache that holds them already (see kv_append); with sinks, or scales by
+    block, marlin_attention_sinks.
 
     q         fp16 [T, q_heads * head_dim], possibly a range of columns;  scale: 1 / sqrt(head_dim) unless given
     window    0, or the number of positions that a token sees, its own included
+    sinks     first positions of a sequence that every token sees besides the window
 
     Returns fp16 [T, q_heads * head_dim]; rows that belong to no sequence are not written."""
     return native().attention_decode(q, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, scale,
-                                     window, out)
+                                     window, out, sinks)
 
 
 def attention_block(A, w_qkv, s_qkv, w_o, s_o, k_cache, v_cache, pages, lengths, K: int, q_heads: int, N: int, group_size: int,
                     workspace, inv_freq=None, interleaved: bool = False, scale=None, window: int = 0, starts=None, k_scale=None,
-                    v_scale=None, QKV=None, Q=None, O=None, out=None, stream=None):
-    """marlin_attention_block: the qkv layer, kv_append, attention_decode and the output layer as four launches; returns
+                    v_scale=None, QKV=None, Q=None, O=None, out=None, stream=None, sinks: int = 0):
+    """marlin_attention_block (with sinks, or scales by block, marlin_attention_block_sinks): the qkv layer, kv_append, attention_decode and the output layer as four launches; returns
     C [M, N].  QKV, Q and O are scratch (taken from torch's allocator unless given)."""
     return native().attention_block(A, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, inv_freq,
-                                    interleaved, scale, window, w_qkv, s_qkv, w_o, s_o, K, q_heads, N, group_size, QKV, Q, O, out)
+                                    interleaved, scale, window, w_qkv, s_qkv, w_o, s_o, K, q_heads, N, group_size, QKV, Q, O, out,
+                                    sinks)
 
 
 class Layer:

@@ -18,8 +18,8 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmarlin_b200.so")
 SOURCES = ["api.cu", "pack.cu", "pack_sparse.cu", "quantize.cu", "gemm_dense.cu", "gemm_tc.cu", "gemm_tc_dense.cu", "gemm_tc_sparse.cu",
-           "gemm_tc_w8.cu", "kv_append.cu", "attention.cu", "attention_tc.cu"]
-HEADERS = [os.path.join(CSRC, "marlin_internal.cuh"), os.path.join(CSRC, "device_utils.cuh"), os.path.join(CSRC, "tc_utils.cuh"), os.path.join(CSRC, "gemm_tc.cuh"), os.path.join(CSRC, "tc_plan.h"), os.path.join(CSRC, "dense_plan.h"), os.path.join(CSRC, "kv_cache.cuh"), os.path.join(CSRC, "attention.cuh"), os.path.join(_ROOT, "include", "marlin_b200.h")]
+           "gemm_tc_w8.cu", "kv_append.cu", "kv_append_blocks.cu", "kv_reserve.cu", "attention.cu", "attention_more.cu", "attention_tc.cu", "attention_tc_more.cu"]
+HEADERS = [os.path.join(CSRC, "marlin_internal.cuh"), os.path.join(CSRC, "device_utils.cuh"), os.path.join(CSRC, "tc_utils.cuh"), os.path.join(CSRC, "gemm_tc.cuh"), os.path.join(CSRC, "tc_plan.h"), os.path.join(CSRC, "dense_plan.h"), os.path.join(CSRC, "kv_cache.cuh"), os.path.join(CSRC, "attention.cuh"), os.path.join(CSRC, "attention_warp.cuh"), os.path.join(CSRC, "attention_tc.cuh"), os.path.join(_ROOT, "include", "marlin_b200.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

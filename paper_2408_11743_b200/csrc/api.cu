@@ -442,12 +442,14 @@ size_t marlin_attention_workspace_bytes(int head_dim) {
   return kWsPartialOff + attention_slot_bytes(head_dim);
 }
 
-// The checks that both calls make of the cache, the tokens and the workspace; on success the cache as the kernels see it.
+// The checks that all calls make of the cache, the tokens and the workspace; on success the cache as the kernels see it.
+// scales: nullptr, or those of the blocks of an 8-bit cache (then c has none)
 static int check_cache(const marlin_kv_cache* c, const int32_t* starts, int tokens, int q_heads, const void* workspace,
-                       size_t workspace_bytes, KvCacheView* view) {
+                       size_t workspace_bytes, KvCacheView* view, const marlin_kv_scales* scales = nullptr) {
+  if (scales && (!scales->k || !scales->v)) return MARLIN_ERR_NULL;
   if (!c || !c->k || !c->v || !c->table || !c->lengths || !workspace) return MARLIN_ERR_NULL;
   const size_t need = marlin_attention_workspace_bytes(c->head_dim);
-  const bool eight_bit = c->format == MARLIN_KV_E4M3;
+  const bool eight_bit = c->format == MARLIN_KV_E4M3 || (scales && c->format == MARLIN_KV_INT8);
   if (!need || (!eight_bit && c->format != MARLIN_KV_FP16) || c->page_size < 1 || (c->page_size & (c->page_size - 1)) ||
       c->pages < 1 || c->max_pages < 1 || c->table_stride < c->max_pages || c->kv_heads < 1 || c->kv_heads > 65536 || c->sequences < 1 ||
       tokens < 1 || (!starts && tokens != c->sequences) || q_heads < 0 || q_heads > 65536 || q_heads % c->kv_heads ||
@@ -464,7 +466,14 @@ static int check_cache(const marlin_kv_cache* c, const int32_t* starts, int toke
                             reinterpret_cast<uintptr_t>(starts) | reinterpret_cast<uintptr_t>(c->k_scale) |
                             reinterpret_cast<uintptr_t>(c->v_scale);
   if (numbers & 3) return MARLIN_ERR_ALIGN;
-  if (!eight_bit && (c->k_scale || c->v_scale)) return MARLIN_ERR_SHAPE;  // a scale that would not be applied
+  if ((!eight_bit || scales) && (c->k_scale || c->v_scale)) return MARLIN_ERR_SHAPE;  // a scale that would not be applied
+  if (scales) {
+    const int block = scales->block_size;
+    if (!eight_bit || block < 1 || block > 128 || (block & (block - 1)) || block > c->page_size || scales->stride[0] < 0 ||
+        scales->stride[1] < 0 || scales->stride[2] < 0)
+      return MARLIN_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(scales->k) | reinterpret_cast<uintptr_t>(scales->v)) & 3) return MARLIN_ERR_ALIGN;
+  }
   if (workspace_bytes < need) return MARLIN_ERR_WORKSPACE;
   view->k = c->k;
   view->v = c->v;
@@ -487,6 +496,25 @@ static int check_cache(const marlin_kv_cache* c, const int32_t* starts, int toke
   return MARLIN_OK;
 }
 
+// the scales of a cache whose checks have passed: those of its blocks, or of its key heads (or none: 1)
+static KvScalesView scales_of(const marlin_kv_cache* c, const marlin_kv_scales* scales) {
+  KvScalesView view = {};
+  if (scales) {
+    view.k = scales->k;
+    view.v = scales->v;
+    view.s_page = scales->stride[0];
+    view.s_head = scales->stride[1];
+    view.s_block = scales->stride[2];
+    while ((1 << view.block_shift) < scales->block_size) ++view.block_shift;
+    view.int8 = c->format == MARLIN_KV_INT8;
+  } else {
+    view.k = const_cast<float*>(c->k_scale);
+    view.v = const_cast<float*>(c->v_scale);
+    view.s_head = 1;
+  }
+  return view;
+}
+
 static int device_is_ours(int* sm_count) {
   DeviceInfo info;
   const int st = device_info(&info);
@@ -497,9 +525,10 @@ static int device_is_ours(int* sm_count) {
 
 static int check_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                         void* q_out, const marlin_kv_cache* cache, const int32_t* starts, int tokens, int q_heads,
-                        const float* inv_freq, int rotary_dim, void* workspace, size_t workspace_bytes, AppendParams* p) {
+                        const float* inv_freq, int rotary_dim, void* workspace, size_t workspace_bytes, AppendParams* p,
+                        const marlin_kv_scales* scales = nullptr) {
   if (!k || !v || (q_heads > 0 && (!q || !q_out))) return MARLIN_ERR_NULL;
-  const int st = check_cache(cache, starts, tokens, q_heads, workspace, workspace_bytes, &p->cache);
+  const int st = check_cache(cache, starts, tokens, q_heads, workspace, workspace_bytes, &p->cache, scales);
   if (st != MARLIN_OK) return st;
   if (q_stride < 0 || k_stride < 0 || v_stride < 0 || (q_heads > 0 && !inv_freq) ||
       (inv_freq && (rotary_dim < 16 || rotary_dim % 16 || rotary_dim > cache->head_dim)))
@@ -519,16 +548,18 @@ static int check_append(const void* q, int64_t q_stride, const void* k, int64_t 
   p->status = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + kWsStatusOff);
   p->q_heads = q_heads;
   p->rotary_dim = rotary_dim;
+  p->tokens = tokens;
+  if (scales) p->scales = scales_of(cache, scales);
   return MARLIN_OK;
 }
 
 static int check_attention(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const int32_t* starts, int tokens,
                            int q_heads, float scale, int window, void* out, void* workspace, size_t workspace_bytes,
-                           AttentionParams* p) {
+                           AttentionParams* p, const marlin_kv_scales* scales = nullptr, int sinks = 0) {
   if (!q || !out) return MARLIN_ERR_NULL;
-  const int st = check_cache(cache, starts, tokens, q_heads, workspace, workspace_bytes, &p->cache);
+  const int st = check_cache(cache, starts, tokens, q_heads, workspace, workspace_bytes, &p->cache, scales);
   if (st != MARLIN_OK) return st;
-  if (q_heads < 1 || window < 0 || q_stride < 0) return MARLIN_ERR_SHAPE;
+  if (q_heads < 1 || window < 0 || sinks < 0 || q_stride < 0) return MARLIN_ERR_SHAPE;
   if (q_stride % 8 || !aligned16(q) || !aligned16(out)) return MARLIN_ERR_ALIGN;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p->q = static_cast<const uint16_t*>(q);
@@ -543,6 +574,7 @@ static int check_attention(const void* q, int64_t q_stride, const marlin_kv_cach
   p->group = q_heads / cache->kv_heads;
   // (a window that no sequence can fill is none)
   p->window = window >= (1 << 30) || window >= (long long)cache->max_pages * cache->page_size ? 0 : window;
+  p->sinks = p->window ? sinks : 0;  // (without a window every position is seen)
   p->scale_log2 = scale * 1.44269504088896340736f;
   // lines of 128 bytes, from the first number to the last; of a table of more than 8 MB, mostly entries that no sequence has
   // reached, the rest stays where it is
@@ -576,10 +608,44 @@ int marlin_attention_decode(const void* q, int64_t q_stride, const marlin_kv_cac
   return launch_attention(p, sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MARLIN_OK : MARLIN_ERR_CUDA;
 }
 
-int marlin_attention_block(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o, void* QKV,
-                           void* Q, void* O, void* C, const marlin_kv_cache* cache, const int32_t* starts, int M, int K,
-                           int q_heads, int N, int group_size, const float* inv_freq, int rotary_dim, int interleaved,
-                           float scale, int window, void* workspace, size_t workspace_bytes, marlin_stream stream) {
+// The kernels for sinks and scales by block take the scales of key heads, too, from where those of blocks lie.
+static void use_scales(AttentionParams* p, const marlin_kv_cache* cache, const marlin_kv_scales* scales) {
+  if (!p->cache.eight_bit) return;
+  p->scales = scales_of(cache, scales);
+  p->cache.k_scale = p->cache.v_scale = nullptr;
+}
+
+int marlin_kv_append_scaled(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            void* q_out, const marlin_kv_cache* cache, const marlin_kv_scales* scales, const int32_t* starts, int tokens,
+                            int q_heads, const float* inv_freq, int rotary_dim, int interleaved, void* workspace, size_t workspace_bytes,
+                            marlin_stream stream) {
+  if (!scales) return MARLIN_ERR_NULL;
+  AppendParams p;
+  int sm_count;
+  int st = check_append(q, q_stride, k, k_stride, v, v_stride, q_out, cache, starts, tokens, q_heads, inv_freq, rotary_dim,
+                        workspace, workspace_bytes, &p, scales);
+  if (st == MARLIN_OK) st = device_is_ours(&sm_count);
+  if (st != MARLIN_OK) return st;
+  return launch_kv_append_blocks(p, interleaved, sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MARLIN_OK : MARLIN_ERR_CUDA;
+}
+
+int marlin_attention_sinks(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const marlin_kv_scales* scales,
+                           const int32_t* starts, int tokens, int q_heads, float scale, int window, int sinks, void* out,
+                           void* workspace, size_t workspace_bytes, marlin_stream stream) {
+  AttentionParams p;
+  int sm_count;
+  int st = check_attention(q, q_stride, cache, starts, tokens, q_heads, scale, window, out, workspace, workspace_bytes, &p, scales, sinks);
+  if (st == MARLIN_OK) st = device_is_ours(&sm_count);
+  if (st != MARLIN_OK) return st;
+  use_scales(&p, cache, scales);
+  return launch_attention_more(p, sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MARLIN_OK : MARLIN_ERR_CUDA;
+}
+
+// `more`: with scales by block, or sinks
+static int attention_block(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o, void* QKV,
+                           void* Q, void* O, void* C, const marlin_kv_cache* cache, const marlin_kv_scales* scales, const int32_t* starts,
+                           int M, int K, int q_heads, int N, int group_size, const float* inv_freq, int rotary_dim, int interleaved,
+                           float scale, int window, int sinks, bool more, void* workspace, size_t workspace_bytes, marlin_stream stream) {
   if (!A || !w_qkv || !s_qkv || !w_o || !s_o || !QKV || (inv_freq && !Q) || !O || !C || !cache) return MARLIN_ERR_NULL;
   const long long head_dim = cache->head_dim, q_cols = q_heads * head_dim, kv_cols = cache->kv_heads * head_dim;
   const long long columns = q_cols + 2 * kv_cols;
@@ -599,17 +665,74 @@ int marlin_attention_block(const void* A, const void* w_qkv, const void* s_qkv, 
   int sm_count;
   int st = check_append(inv_freq ? QKV : nullptr, columns, qkv + q_cols, columns, qkv + q_cols + kv_cols, columns,
                         inv_freq ? Q : nullptr, cache, starts, M, inv_freq ? q_heads : 0, inv_freq, rotary_dim, workspace,
-                        workspace_bytes, &append);
+                        workspace_bytes, &append, scales);
   if (st == MARLIN_OK)
-    st = check_attention(q, q_stride, cache, starts, M, q_heads, scale, window, O, workspace, workspace_bytes, &attention);
+    st = check_attention(q, q_stride, cache, starts, M, q_heads, scale, window, O, workspace, workspace_bytes, &attention, scales,
+                         sinks);
+  if (more) use_scales(&attention, cache, scales);
   if (st == MARLIN_OK) st = device_is_ours(&sm_count);
   if (st == MARLIN_OK)
     st = marlin_gemm(A, w_qkv, s_qkv, QKV, M, K, (int)columns, group_size, workspace, workspace_bytes, stream);
   if (st != MARLIN_OK) return st;
-  if (launch_kv_append(append, M, interleaved, sm_count, static_cast<cudaStream_t>(stream)) != cudaSuccess ||
-      launch_attention(attention, sm_count, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((scales ? launch_kv_append_blocks(append, interleaved, sm_count, s) : launch_kv_append(append, M, interleaved, sm_count, s)) != cudaSuccess ||
+      (more ? launch_attention_more(attention, sm_count, s) : launch_attention(attention, sm_count, s)) != cudaSuccess)
     return MARLIN_ERR_CUDA;
   return marlin_gemm(O, w_o, s_o, C, M, (int)q_cols, N, group_size, workspace, workspace_bytes, stream);
+}
+
+int marlin_attention_block(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o, void* QKV,
+                           void* Q, void* O, void* C, const marlin_kv_cache* cache, const int32_t* starts, int M, int K,
+                           int q_heads, int N, int group_size, const float* inv_freq, int rotary_dim, int interleaved,
+                           float scale, int window, void* workspace, size_t workspace_bytes, marlin_stream stream) {
+  return attention_block(A, w_qkv, s_qkv, w_o, s_o, QKV, Q, O, C, cache, nullptr, starts, M, K, q_heads, N, group_size, inv_freq,
+                         rotary_dim, interleaved, scale, window, 0, false, workspace, workspace_bytes, stream);
+}
+
+int marlin_attention_block_sinks(const void* A, const void* w_qkv, const void* s_qkv, const void* w_o, const void* s_o, void* QKV,
+                                 void* Q, void* O, void* C, const marlin_kv_cache* cache, const marlin_kv_scales* scales,
+                                 const int32_t* starts, int M, int K, int q_heads, int N, int group_size, const float* inv_freq,
+                                 int rotary_dim, int interleaved, float scale, int window, int sinks, void* workspace,
+                                 size_t workspace_bytes, marlin_stream stream) {
+  return attention_block(A, w_qkv, s_qkv, w_o, s_o, QKV, Q, O, C, cache, scales, starts, M, K, q_heads, N, group_size, inv_freq,
+                         rotary_dim, interleaved, scale, window, sinks, true, workspace, workspace_bytes, stream);
+}
+
+int marlin_kv_reserve(const marlin_kv_pages* c, const int32_t* counts, const int32_t* keep, int tokens, int32_t* starts, int64_t* slots,
+                      int32_t* positions, void* workspace, size_t workspace_bytes, marlin_stream stream) {
+  if (!c || !c->table || !c->lengths || !c->free_pages || !c->free_count || !workspace) return MARLIN_ERR_NULL;
+  if (c->page_size < 1 || (c->page_size & (c->page_size - 1)) || c->page_size > (1 << 30) || c->max_pages < 1 || c->table_stride < c->max_pages ||
+      c->sequences < 1 || c->capacity < 1 || tokens < 0 || tokens > (1 << 30))
+    return MARLIN_ERR_SHAPE;
+  const uintptr_t numbers = reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->lengths) |
+                            reinterpret_cast<uintptr_t>(c->free_pages) | reinterpret_cast<uintptr_t>(c->free_count) |
+                            reinterpret_cast<uintptr_t>(counts) | reinterpret_cast<uintptr_t>(keep) |
+                            reinterpret_cast<uintptr_t>(starts) | reinterpret_cast<uintptr_t>(positions);
+  if ((numbers & 3) || (reinterpret_cast<uintptr_t>(slots) & 7) || !aligned16(workspace)) return MARLIN_ERR_ALIGN;
+  if (workspace_bytes < kWsPartialOff) return MARLIN_ERR_WORKSPACE;
+  int sm_count;
+  const int st = device_is_ours(&sm_count);
+  if (st != MARLIN_OK) return st;
+  ReserveParams p;
+  p.lengths = c->lengths;
+  p.table = c->table;
+  p.table_stride = c->table_stride;
+  p.free_pages = c->free_pages;
+  p.free_count = c->free_count;
+  p.counts = counts;
+  p.keep = keep;
+  p.starts = starts;
+  p.slots = reinterpret_cast<long long*>(slots);
+  p.positions = positions;
+  p.status = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + kWsStatusOff);
+  p.counter = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + kWsCounterOff);
+  p.capacity = c->capacity;
+  p.max_pages = c->max_pages;
+  p.sequences = c->sequences;
+  p.page_shift = 0;
+  while ((1 << p.page_shift) < c->page_size) ++p.page_shift;
+  p.tokens = tokens;
+  return launch_kv_reserve(p, sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MARLIN_OK : MARLIN_ERR_CUDA;
 }
 
 int marlin_read_status(const void* workspace, marlin_stream stream) {

@@ -2,6 +2,8 @@
 #pragma once
 #include <limits.h>
 
+#include <type_traits>
+
 #include "kv_cache.cuh"
 
 namespace marlin_b200 {
@@ -22,8 +24,18 @@ constexpr float kNone = -INFINITY;
 constexpr float kBelow = 7.f;
 constexpr float kSlack = 15.f;
 
+// What a call may have beside a window and scales per key head, as an argument of the kernels' templates, so that calls without it stay as
+// they are.  kExtra: first positions that stay visible in front of a window (sinks), blocks of rows that have tiles of their
+// own, and, over 8 bits, a scale for each block of tokens and key head; kExtraInt8: the same with codes in two's complement.
+enum Extra { kNoExtra, kExtra, kExtraInt8 };
+
 constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
+// the same of four bytes, through the L1: neighbours in a table of scales are asked for one after the other
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+  const int bytes = there ? 4 : 0;
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   const int bytes = there ? 16 : 0;  // the rest is filled with zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -105,9 +117,12 @@ __device__ __forceinline__ void prefetch_table(const AttentionParams& p, int thr
 
 // What a sequence asks for: new tokens [first, first + n) of the call, tiles [tile0, tile0 + tiles) of its len keys, blocks of
 // rows per key head.  A sequence with new tokens has a tile at least: it writes the zeros.
+// (Extra: every block of rows has as many tiles as the one that needs most of them, the tiles of the sinks, `sinks` of them, in
+// front; where the others begin is its own, see Range::next.)
 struct Sequence {
-  int len, n, first, tile0, tiles, blocks;
+  int len, n, first, tile0, tiles, blocks, sinks;
 };
+template <int EXTRA = kNoExtra>
 __device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, int rows, int tile, bool& bad) {
   Sequence s;
   s.len = cache_length(p.cache, b, bad);
@@ -118,9 +133,24 @@ __device__ __forceinline__ Sequence sequence(const AttentionParams& p, int b, in
     s.first = from;
     s.n = to - from;
   }
+  s.blocks = (s.n * p.group + rows - 1) / rows;
+  if (EXTRA != kNoExtra) {
+    const int total = max(1, (s.len + tile - 1) / tile);
+    s.tile0 = s.sinks = 0;
+    s.tiles = total;
+    if (p.window) {
+      s.sinks = min(total, (min(p.sinks, s.len) + tile - 1) / tile);
+      if (s.blocks <= 1) {
+        s.tiles = s.sinks + total - max(s.sinks, max(0, s.len - s.n - p.window + 1) / tile);
+      } else {  // tokens that the rows of a block can belong to, keys that these see, tiles that so many keys can lie in
+        const int tokens = rows % p.group ? (rows + p.group - 2) / p.group + 1 : rows / p.group, keys = p.window + tokens - 1;
+        s.tiles = min(total, s.sinks + (keys + tile - 2) / tile + 1);
+      }
+    }
+    return s;
+  }
   s.tile0 = (p.window ? max(0, s.len - s.n - p.window + 1) : 0) / tile;
   s.tiles = max(1, (s.len + tile - 1) / tile - s.tile0);
-  s.blocks = (s.n * p.group + rows - 1) / rows;
   return s;
 }
 
@@ -150,6 +180,20 @@ struct Stripes {
 struct Segment {
   int b, h, tile, nt, row0, rows, base_high, n, first, c0, c1;
 };
+// Extra: x.tile counts from the first tile of the item; of these the first `sinks` are the first of the sequence, the others lie `gap`
+// further on.  (A row then sees the positions below `sinks` of the call, too.)
+struct SegmentWithGap : Segment {
+  int sinks, gap;
+};
+template <int EXTRA>
+using SegmentOf = std::conditional_t<EXTRA == kNoExtra, Segment, SegmentWithGap>;
+// tile i of the segment, in tiles of the sequence
+template <int EXTRA>
+__device__ __forceinline__ int tile_of(const SegmentOf<EXTRA>& x, int i) {
+  int t = x.tile + i;
+  if constexpr (EXTRA != kNoExtra) t += t >= x.sinks ? x.gap : 0;
+  return t;
+}
 // positions that some row of a segment sees: [low_min, high_max), that all of them see: [low_max, high_min)
 struct Visible {
   int low_min, low_max, high_min, high_max;
@@ -168,7 +212,7 @@ __device__ __forceinline__ Visible visible(const AttentionParams& p, const Segme
 
 // The segments of this CTA's range one after the other, as a whole warp follows them.  ROWS: of a block; TILE: keys of a tile;
 // LEAD: what an item costs beside its tiles, in tiles.
-template <int ROWS, int TILE, int LEAD>
+template <int ROWS, int TILE, int LEAD, int EXTRA = kNoExtra>
 struct Range {
   Stripes stripes;
   Sequence s;
@@ -184,7 +228,7 @@ struct Range {
     uint32_t mine = 0;
     bool bad = false;
     for (int i = lane * per; i < min(c.sequences, (lane + 1) * per); ++i) {
-      const Sequence s = sequence(p, i, ROWS, TILE, bad);
+      const Sequence s = sequence<EXTRA>(p, i, ROWS, TILE, bad);
       const unsigned long long units = (unsigned long long)c.kv_heads * s.blocks * (s.tiles + LEAD) + mine;
       mine = (uint32_t)min(units, (unsigned long long)kMostUnits);
     }
@@ -220,7 +264,7 @@ struct Range {
       b = owner * per;
       uint32_t off = at - __shfl_sync(~0u, before, owner);
       for (;; ++b) {
-        s = sequence(p, b, ROWS, TILE, bad);
+        s = sequence<EXTRA>(p, b, ROWS, TILE, bad);
         const uint32_t units = (uint32_t)c.kv_heads * s.blocks * (s.tiles + LEAD);
         if (off < units) break;
         off -= units;
@@ -235,7 +279,7 @@ struct Range {
   }
 
   // the next one; nt = 0: there is none
-  __device__ __forceinline__ Segment next(const AttentionParams& p) {
+  __device__ __forceinline__ SegmentOf<EXTRA> next(const AttentionParams& p) {
     const KvCacheView& c = p.cache;
     if (more && skip == (uint32_t)s.tiles + LEAD) {
       more = at < end;
@@ -244,12 +288,12 @@ struct Range {
         if (++item == c.kv_heads * s.blocks) {
           item = 0;
           bool bad = false;  // (reported by begin())
-          do s = sequence(p, ++b, ROWS, TILE, bad);
+          do s = sequence<EXTRA>(p, ++b, ROWS, TILE, bad);
           while (s.blocks == 0);
         }
       }
     }
-    Segment x = {};
+    SegmentOf<EXTRA> x = {};
     if (more) {
       const uint32_t i0 = at - skip, i1 = i0 + LEAD + s.tiles, to = min(stripes.moved(end, i0, i1), i1);
       if (at < to) {
@@ -263,6 +307,12 @@ struct Range {
         x.base_high = s.len - s.n + 1;
         x.n = s.n;
         x.first = s.first;
+        if constexpr (EXTRA != kNoExtra) {  // (as many tiles as there are for every block: the last ones end with the sequence)
+          const int low = p.window ? max(0, x.base_high + x.row0 / p.group - p.window) : 0;
+          const int last = max(1, (s.len + TILE - 1) / TILE) - (s.tiles - s.sinks);
+          x.sinks = s.sinks;
+          x.gap = min(max(low / TILE, s.sinks), last) - s.sinks;
+        }
         uint32_t c0 = blockIdx.x, c1 = blockIdx.x;
         if (x.nt != s.tiles) {
           c0 = stripes.owner(i0);
@@ -296,6 +346,21 @@ __device__ __forceinline__ void write_four(const AttentionParams& p, const Segme
   *reinterpret_cast<uint2*>(p.out + ((long long)(x.first + token) * p.q_heads + head) * p.cache.head_dim + d) = two;
 }
 
+// The value of element d at position pos of (sequence b, head h) if it is not finite, otherwise 0.
+template <bool F8>
+__device__ __forceinline__ float if_not_finite(const AttentionParams& p, int b, int h, int pos, int d) {
+  const KvCacheView& c = p.cache;
+  const long long off = cache_offset(c, load(c.table + b * c.table_stride + (pos >> c.page_shift)), h, pos, p.status);
+  if (off < 0) return 0.f;
+  float v;
+  if (F8) {
+    const uint32_t two = e4m3x2_to_f16x2(static_cast<const uint8_t*>(c.v)[off + d]);
+    v = __low2float(*reinterpret_cast<const __half2*>(&two));
+  } else {
+    v = __half2float(static_cast<const __half*>(c.v)[off + d]);
+  }
+  return isfinite(v) ? 0.f : v;
+}
 // What was left out of the products of a segment, for element d of row r: the values that are not finite among the keys that some rows
 // see and others do not.
 template <bool F8>
@@ -310,18 +375,52 @@ __device__ __forceinline__ float not_finite_sum(const AttentionParams& p, const 
       pos = sees.high_min - 1;
       continue;
     }
-    const long long off = cache_offset(c, load(c.table + x.b * c.table_stride + (pos >> c.page_shift)), x.h, pos, p.status);
-    if (off < 0) continue;
-    float v;
-    if (F8) {
-      const uint32_t two = e4m3x2_to_f16x2(static_cast<const uint8_t*>(c.v)[off + d]);
-      v = __low2float(*reinterpret_cast<const __half2*>(&two));
-    } else {
-      v = __half2float(static_cast<const __half*>(c.v)[off + d]);
-    }
-    if (!isfinite(v)) sum += v;
+    sum += if_not_finite<F8>(p, x.b, x.h, pos, d);
   }
   return sum;
+}
+// The same with sinks, which every row sees: from the edge of the window, as far as they are not sinks, and around the new tokens.
+template <bool F8>
+__device__ __forceinline__ float not_finite_sum(const AttentionParams& p, const SegmentWithGap& x, const Visible& sees, int tile_keys, int r, int d) {
+  const int high = x.base_high + token_of(p, x, r), low = p.window ? max(0, high - p.window) : 0;
+  float sum = 0.f;
+  if (d >= p.cache.head_dim) return sum;
+#pragma unroll 1
+  for (int part = 0; part < 2; ++part) {
+    const int from = part ? sees.high_min : max(sees.low_min, p.sinks), to = part ? sees.high_max : min(sees.low_max, sees.high_min);
+#pragma unroll 1
+    for (int pos = max(from, 0); pos < to; ++pos) {
+      const int tile = pos / tile_keys, at = tile < x.sinks ? tile : tile - x.gap;
+      const bool here = (tile < x.sinks || tile >= x.sinks + x.gap) && at >= x.tile && at < x.tile + x.nt;
+      if (here && pos < high && (pos >= low || pos < p.sinks)) sum += if_not_finite<F8>(p, x.b, x.h, pos, d);
+    }
+  }
+  return sum;
+}
+// Whether some row of a segment sees a key: from its window on, or among the sinks.
+template <int EXTRA>
+__device__ __forceinline__ bool seen_by_some(const AttentionParams& p, int key, int low, int high) {
+  return key < high && (key >= low || (EXTRA != kNoExtra && key < p.sinks));
+}
+// Whether all of `count` keys from key0 on are (all in the window or all sinks).
+template <int EXTRA>
+__device__ __forceinline__ bool all_seen_by_some(const AttentionParams& p, int key0, int count, int low, int high) {
+  return key0 + count <= high && (key0 >= low || (EXTRA != kNoExtra && key0 + count <= p.sinks));
+}
+// where the scale of a token lies, from the number of its page (which is there)
+__device__ __forceinline__ long long scale_offset(const AttentionParams& p, int page, int h, int pos) {
+  const KvScalesView& s = p.scales;
+  return page * s.s_page + h * s.s_head + ((pos & ((1 << p.cache.page_shift) - 1)) >> s.block_shift) * s.s_block;
+}
+static __device__ const float kScaleOfOne = 1.f;  // where a cache has no scales
+// The least power of two that is not below x > 0, between 2^-126 and 2^127.
+__device__ __forceinline__ float power_above(float x) {
+  const uint32_t bits = __float_as_uint(x), up = (bits & 0x7f800000u) + (bits & 0x7fffffu ? 0x800000u : 0u);
+  return __uint_as_float(min(max(up, 0x800000u), 254u << 23));
+}
+__device__ __forceinline__ float finite_or_zero(float x) {  // its magnitude
+  x = fabsf(x);
+  return x <= 3.402823466e38f ? x : 0.f;
 }
 
 // ---- parts of an item in the workspace -----------------------------------------------------------

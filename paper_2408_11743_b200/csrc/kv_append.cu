@@ -48,25 +48,6 @@ __device__ __forceinline__ Unit unit_of(const AppendParams& p, int u) {
   return r;
 }
 
-__device__ __forceinline__ void to_floats(uint4 v, float (&x)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
-}
-__device__ __forceinline__ uint4 to_halves(const float (&x)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 template <bool F8>
 __device__ __forceinline__ void store_cache(void* base, long long off, const float (&x)[8], float scale) {
   if (F8) {

@@ -64,4 +64,30 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
   return r;
 }
 
+__device__ __forceinline__ void to_floats(uint4 v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+__device__ __forceinline__ uint4 to_halves(const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// bytes of a word of codes in two's complement -> fp16, exact: a code + 128 under the exponent of 1024, less 1152.
+// x: the word with its sign bits turned (int8_biased); `select`: which two bytes (0x4140: the lower ones, 0x4342: the upper ones)
+__device__ __forceinline__ uint32_t int8_biased(uint32_t word) { return word ^ 0x80808080u; }
+__device__ __forceinline__ uint32_t int8x2_to_f16x2(uint32_t x, uint32_t select) {
+  return hsub2_u32(__byte_perm(x, 0x64646464u, select), 0x64806480u);
+}
+
 }  // namespace marlin_b200

@@ -131,6 +131,15 @@ struct KvCacheView {
   int eight_bit;
 };
 
+// scales of an 8-bit cache, one per block of 2^block_shift tokens of a page and key head: scale of (page, head, block) at
+// page * s_page + head * s_head + block * s_block.  All strides but s_head 0: one per key head
+struct KvScalesView {
+  float *k, *v;          // nullptr: 1 (per key head only)
+  long long s_page, s_head, s_block;
+  int block_shift;
+  int int8;              // codes are two's complement, not e4m3
+};
+
 struct AppendParams {
   KvCacheView cache;
   const uint16_t *q, *k, *v;
@@ -143,8 +152,29 @@ struct AppendParams {
   // filled in by the launch: units of a token, of a query or key head, of those its pairs; units that a thread takes
   int units, head_units, pair_units, units_per_thread;
   uint32_t head_magic, value_magic;  // for divisions by head_units and by head_dim / 8 (kv_append.cu)
+  KvScalesView scales;   // kv_append_blocks.cu
+  int tokens;
 };
 cudaError_t launch_kv_append(AppendParams p, int tokens, int interleaved, int sm_count, cudaStream_t stream);
+// the same into an 8-bit cache with a scale for each block of tokens and key head (kv_append_blocks.cu)
+cudaError_t launch_kv_append_blocks(AppendParams p, int interleaved, int sm_count, cudaStream_t stream);
+
+// page tables from lengths (kv_reserve.cu)
+struct ReserveParams {
+  int* lengths;
+  int* table;
+  long long table_stride;
+  int* free_pages;
+  int* free_count;
+  const int *counts, *keep;  // or nullptr: one new token each; everything is kept
+  int* starts;               // out, or nullptr
+  long long* slots;          // out, or nullptr
+  int* positions;            // out, or nullptr
+  int* status;
+  int* counter;
+  int capacity, max_pages, sequences, page_shift, tokens;
+};
+cudaError_t launch_kv_reserve(const ReserveParams& p, int sm_count, cudaStream_t stream);
 
 struct AttentionParams {
   KvCacheView cache;
@@ -159,12 +189,17 @@ struct AttentionParams {
   int window;            // 0: none
   float scale_log2;      // scale * log2(e)
   int table_lines;   // of the page table: asked for before anything else
+  int sinks;             // first positions that every token sees (with a window only)
+  KvScalesView scales;   // kExtra, kExtraInt8
 };
 size_t attention_slot_bytes(int head_dim);
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream);
 // head_dim up to 128, where a key head has more than eight rows of an fp16 cache, or more than 32 of 128 elements of an 8-bit one
 // (launch_rows in attention.cu; the kernel is in attention_tc.cu)
 cudaError_t launch_attention_tc(const AttentionParams& p, int sm_count, cudaStream_t stream);
+// the same with sinks and with scales by block (attention_more.cu, attention_tc_more.cu); an 8-bit cache has its scales in p.scales
+cudaError_t launch_attention_more(const AttentionParams& p, int sm_count, cudaStream_t stream);
+cudaError_t launch_attention_tc_more(const AttentionParams& p, int sm_count, cudaStream_t stream);
 
 // ---- the stripe partition (host and device use the same two formulas) ------------------------
 // worker w of P owns units [w*U/P, (w+1)*U/P); the owner of unit x is floor(((x+1)*P - 1) / U).

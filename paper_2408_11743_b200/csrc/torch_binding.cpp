@@ -38,6 +38,10 @@ MlpFn g_mlp;
 decltype(&marlin_kv_append) g_append;
 decltype(&marlin_attention_decode) g_attention;
 decltype(&marlin_attention_block) g_block;
+decltype(&marlin_kv_append_scaled) g_append_scaled;
+decltype(&marlin_attention_sinks) g_attention_sinks;
+decltype(&marlin_attention_block_sinks) g_block_sinks;
+decltype(&marlin_kv_reserve) g_reserve;
 SizeFn g_weight_bytes, g_scale_bytes;
 SizeFn2 g_meta_bytes, g_weight_bytes_w8;
 PyObject* g_raise;  // raise(status, what)
@@ -297,7 +301,7 @@ PyObject* mlp(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 
 // ---- the paged key-value cache ------------------------------------------------------------------------------------
 const char* type_name(at::ScalarType type) {
-  return type == at::kHalf ? "torch.float16" : type == at::kInt ? "torch.int32" : type == at::kFloat ? "torch.float32" : "torch.uint8";
+  return type == at::kHalf ? "torch.float16" : type == at::kInt ? "torch.int32" : type == at::kLong ? "torch.int64" : type == at::kFloat ? "torch.float32" : "torch.uint8";
 }
 // `o` as a tensor of this type and these sizes (-1: any) on `device`, its elements side by side in the last dimension (and in
 // all where `dense`); nullptr with a Python error set
@@ -332,9 +336,24 @@ const at::Tensor* argument(PyObject* o, const char* name, at::ScalarType type, s
 // a row stride: of a single row it means nothing
 int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
 
+// The stream of a call: the one that is given, or the current one of the device of its tensors, which becomes the current device.
+bool on_stream_of(PyObject* given, c10::DeviceIndex index, void** stream, std::optional<c10::cuda::CUDAGuard>* on_device,
+                  std::optional<c10::cuda::CUDAStreamGuard>* on_stream) {
+  if (given == Py_None) {
+    if (c10::cuda::current_device() != index) on_device->emplace(index);
+    *stream = c10::cuda::getCurrentCUDAStream(index).stream();
+  } else {
+    if (!stream_handle(given, stream)) return false;
+    on_stream->emplace(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(*stream), index));
+  }
+  return true;
+}
+
 // the arguments that all calls on a cache have: (k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream)
 struct CacheCall {
   marlin_kv_cache c{};
+  marlin_kv_scales by_block{};  // of an 8-bit cache with scales by block
+  const marlin_kv_scales* scales = nullptr;  // that, or none
   const int32_t* starts = nullptr;
   void* workspace;
   size_t workspace_bytes;
@@ -357,8 +376,10 @@ bool cache_arguments(PyObject* const* a, CacheCall* out) {
     c.format = MARLIN_KV_FP16;
   } else if (k->scalar_type() == at::kFloat8_e4m3fn) {
     c.format = MARLIN_KV_E4M3;
+  } else if (k->scalar_type() == at::kChar) {
+    c.format = MARLIN_KV_INT8;
   } else {
-    PyErr_SetString(PyExc_TypeError, "k_cache must have dtype torch.float16 or torch.float8_e4m3fn");
+    PyErr_SetString(PyExc_TypeError, "k_cache must have dtype torch.float16, torch.float8_e4m3fn or torch.int8");
     return false;
   }
   if (v->scalar_type() != k->scalar_type() || v->device() != k->device() || k->dim() != 4 || k->sizes() != v->sizes() ||
@@ -408,25 +429,50 @@ bool cache_arguments(PyObject* const* a, CacheCall* out) {
     out->starts = static_cast<const int32_t*>(t->data_ptr());
   }
   static const char* const names[2] = {"k_scale", "v_scale"};
+  // scales by block, [pages, kv_heads, blocks of a page], of keys and values alike; or one per key head
+  const bool three[2] = {a[6] != Py_None && THPVariable_Check(a[6]) && THPVariable_Unpack(a[6]).dim() == 3,
+                         a[7] != Py_None && THPVariable_Check(a[7]) && THPVariable_Unpack(a[7]).dim() == 3};
+  const bool by_block = three[0] || three[1] || c.format == MARLIN_KV_INT8;
+  const at::Tensor* by[2] = {};
   for (int i = 0; i < 2; ++i) {
     if (a[6 + i] == Py_None) continue;
-    if (c.format != MARLIN_KV_E4M3) {
+    if (c.format == MARLIN_KV_FP16) {
       PyErr_Format(PyExc_ValueError, "%s is for 8-bit caches", names[i]);
       return false;
+    }
+    if (by_block) {
+      by[i] = argument(a[6 + i], names[i], at::kFloat, {k->size(0), k->size(1), -1}, out->device, false);
+      if (!by[i]) return false;
+      continue;
     }
     const at::Tensor* t = argument(a[6 + i], names[i], at::kFloat, {k->size(1)}, out->device, true);
     if (!t) return false;
     (i ? c.v_scale : c.k_scale) = static_cast<const float*>(t->data_ptr());
   }
-  const c10::DeviceIndex index = out->device.index();
-  if (a[8] == Py_None) {
-    if (c10::cuda::current_device() != index) out->on_device.emplace(index);
-    out->stream = c10::cuda::getCurrentCUDAStream(index).stream();
-  } else {
-    if (!stream_handle(a[8], &out->stream)) return false;
-    out->on_stream.emplace(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(out->stream), index));
+  if (by_block) {
+    if (!by[0] || !by[1]) {
+      PyErr_SetString(PyExc_ValueError, "k_scale and v_scale must both be [pages, kv_heads, page_size / block]");
+      return false;
+    }
+    const int64_t blocks = by[0]->size(2);
+    if (by[0]->sizes() != by[1]->sizes() || by[0]->strides() != by[1]->strides() || blocks < 1 || k->size(2) % blocks) {
+      PyErr_SetString(PyExc_ValueError, "k_scale and v_scale must be [pages, kv_heads, page_size / block] alike");
+      return false;
+    }
+    marlin_kv_scales& s = out->by_block;
+    for (int i = 0; i < 3; ++i) {
+      s.stride[i] = by[0]->size(i) > 1 ? by[0]->stride(i) : 0;
+      if (by[0]->size(i) > 1 && by[0]->stride(i) < 1) {
+        PyErr_SetString(PyExc_ValueError, "k_scale: scales overlap");
+        return false;
+      }
+    }
+    s.k = static_cast<float*>(by[0]->data_ptr());
+    s.v = static_cast<float*>(by[1]->data_ptr());
+    s.block_size = (int)(k->size(2) / blocks);
+    out->scales = &s;
   }
-  return true;
+  return on_stream_of(a[8], out->device.index(), &out->stream, &out->on_device, &out->on_stream);
 }
 // rows of heads, [T, heads * head_dim]; `o` may be a range of columns of a wider tensor
 const at::Tensor* rows_of_heads(PyObject* o, const char* name, const CacheCall& call, int* tokens, int64_t* heads) {
@@ -496,10 +542,15 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   void* to = turn ? out.data_ptr() : nullptr;
   int st;
   Py_BEGIN_ALLOW_THREADS
-  st = g_append(turn ? p : nullptr, stride, p + q_heads * D, stride, p + (q_heads + kv) * D, stride, to, &call.c, call.starts, tokens,
-                turn ? (int)q_heads : 0, inv_freq, rotary_dim, interleaved, call.workspace, call.workspace_bytes, call.stream);
+  if (call.scales)
+    st = g_append_scaled(turn ? p : nullptr, stride, p + q_heads * D, stride, p + (q_heads + kv) * D, stride, to, &call.c, call.scales,
+                         call.starts, tokens, turn ? (int)q_heads : 0, inv_freq, rotary_dim, interleaved, call.workspace,
+                         call.workspace_bytes, call.stream);
+  else
+    st = g_append(turn ? p : nullptr, stride, p + q_heads * D, stride, p + (q_heads + kv) * D, stride, to, &call.c, call.starts, tokens,
+                  turn ? (int)q_heads : 0, inv_freq, rotary_dim, interleaved, call.workspace, call.workspace_bytes, call.stream);
   Py_END_ALLOW_THREADS
-  return finish(st, "marlin_kv_append", a[12], std::move(out));
+  return finish(st, call.scales ? "marlin_kv_append_scaled" : "marlin_kv_append", a[12], std::move(out));
   CATCH
 }
 
@@ -514,43 +565,49 @@ bool softmax_arguments(PyObject* scale_o, PyObject* window_o, int head_dim, floa
   return integer(window_o, "window", window);
 }
 
-// attention_decode(q, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, scale, window, out)
+// attention_decode(q, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, scale, window, out, sinks)
 PyObject* attention_decode(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   TRY
-  if (!count_is(nargs, 13)) return nullptr;
+  if (!count_is(nargs, 14)) return nullptr;
   CacheCall call;
   if (!cache_arguments(a + 1, &call)) return nullptr;
-  int tokens, window;
+  int tokens, window, sinks;
   int64_t heads;
   float scale;
   const at::Tensor* q = rows_of_heads(a[0], "q", call, &tokens, &heads);
-  if (!q || !softmax_arguments(a[10], a[11], call.c.head_dim, &scale, &window)) return nullptr;
+  if (!q || !softmax_arguments(a[10], a[11], call.c.head_dim, &scale, &window) || !integer(a[13], "sinks", &sinks)) return nullptr;
   at::Tensor out;
   if (!same_device(a[12], call, "out") || !output(a[12], tokens, heads * call.c.head_dim, call.device, "out", &out)) return nullptr;
   const void* p = q->data_ptr();
   void* to = out.data_ptr();
   const int64_t stride = row_stride(*q);
+  const bool more = call.scales || sinks != 0;
   int st;
   Py_BEGIN_ALLOW_THREADS
-  st = g_attention(p, stride, &call.c, call.starts, tokens, (int)heads, scale, window, to, call.workspace, call.workspace_bytes,
-                   call.stream);
+  if (more)
+    st = g_attention_sinks(p, stride, &call.c, call.scales, call.starts, tokens, (int)heads, scale, window, sinks, to, call.workspace,
+                           call.workspace_bytes, call.stream);
+  else
+    st = g_attention(p, stride, &call.c, call.starts, tokens, (int)heads, scale, window, to, call.workspace, call.workspace_bytes,
+                     call.stream);
   Py_END_ALLOW_THREADS
-  return finish(st, "marlin_attention_decode", a[12], std::move(out));
+  return finish(st, more ? "marlin_attention_sinks" : "marlin_attention_decode", a[12], std::move(out));
   CATCH
 }
 
 // attention_block(A, k_cache, v_cache, pages, lengths, workspace, starts, k_scale, v_scale, stream, inv_freq, interleaved, scale,
-//                 window, w_qkv, s_qkv, w_o, s_o, K, q_heads, N, G, QKV, Q, O, out)
+//                 window, w_qkv, s_qkv, w_o, s_o, K, q_heads, N, G, QKV, Q, O, out, sinks)
 PyObject* attention_block(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   TRY
-  if (!count_is(nargs, 26)) return nullptr;
+  if (!count_is(nargs, 27)) return nullptr;
   CacheCall call;
   if (!cache_arguments(a + 1, &call)) return nullptr;
-  int K, q_heads, N, G, window, rotary_dim;
+  int K, q_heads, N, G, window, sinks, rotary_dim;
   float scale;
   const float* inv_freq;
   if (!frequencies(a[10], call, &inv_freq, &rotary_dim) || !softmax_arguments(a[12], a[13], call.c.head_dim, &scale, &window) ||
-      !integer(a[18], "K", &K) || !integer(a[19], "q_heads", &q_heads) || !integer(a[20], "N", &N) || !integer(a[21], "group_size", &G))
+      !integer(a[18], "K", &K) || !integer(a[19], "q_heads", &q_heads) || !integer(a[20], "N", &N) || !integer(a[21], "group_size", &G) ||
+      !integer(a[26], "sinks", &sinks))
     return nullptr;
   const int interleaved = PyObject_IsTrue(a[11]);
   if (interleaved < 0) return nullptr;
@@ -581,12 +638,90 @@ PyObject* attention_block(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const void *pa = A->data_ptr(), *p[4];
   for (int i = 0; i < 4; ++i) p[i] = t[i]->data_ptr();
   void *pqkv = QKV.data_ptr(), *pq = inv_freq ? Q.data_ptr() : nullptr, *po = O.data_ptr(), *pc = out.data_ptr();
+  const bool more = call.scales || sinks != 0;
   int st;
   Py_BEGIN_ALLOW_THREADS
-  st = g_block(pa, p[0], p[1], p[2], p[3], pqkv, pq, po, pc, &call.c, call.starts, (int)M, K, q_heads, N, G, inv_freq, rotary_dim,
-               interleaved, scale, window, call.workspace, call.workspace_bytes, call.stream);
+  if (more)
+    st = g_block_sinks(pa, p[0], p[1], p[2], p[3], pqkv, pq, po, pc, &call.c, call.scales, call.starts, (int)M, K, q_heads, N, G, inv_freq,
+                       rotary_dim, interleaved, scale, window, sinks, call.workspace, call.workspace_bytes, call.stream);
+  else
+    st = g_block(pa, p[0], p[1], p[2], p[3], pqkv, pq, po, pc, &call.c, call.starts, (int)M, K, q_heads, N, G, inv_freq, rotary_dim,
+                 interleaved, scale, window, call.workspace, call.workspace_bytes, call.stream);
   Py_END_ALLOW_THREADS
-  return finish(st, "marlin_attention_block", a[25], std::move(out));
+  return finish(st, more ? "marlin_attention_block_sinks" : "marlin_attention_block", a[25], std::move(out));
+  CATCH
+}
+
+// an output of a call, in one dimension: `given`, or a new one
+bool vector_output(PyObject* given, int64_t n, at::ScalarType type, const at::Device& device, const char* name, at::Tensor* out) {
+  if (given == Py_None) {
+    *out = at::Tensor(at::detail::empty_cuda({n}, type, device, std::nullopt));
+    return true;
+  }
+  const at::Tensor* t = argument(given, name, type, {n}, device, true);
+  if (t) *out = *t;
+  return t != nullptr;
+}
+
+// kv_reserve(lengths, pages, free_pages, free_count, workspace, page_size, tokens, counts, keep, starts, slots, positions, stream)
+PyObject* kv_reserve(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  TRY
+  if (!count_is(nargs, 13)) return nullptr;
+  const at::Tensor* lengths = tensor(a[0], "lengths");
+  if (!lengths) return nullptr;
+  const at::Device device = lengths->device();
+  if (!(lengths = argument(a[0], "lengths", at::kInt, {-1}, device, true))) return nullptr;
+  const int64_t sequences = lengths->size(0);
+  const at::Tensor* table = argument(a[1], "pages", at::kInt, {sequences, -1}, device, false);
+  if (!table) return nullptr;
+  const at::Tensor* free_pages = argument(a[2], "free_pages", at::kInt, {-1}, device, true);
+  if (!free_pages) return nullptr;
+  const at::Tensor* free_count = argument(a[3], "free_count", at::kInt, {1}, device, true);
+  if (!free_count) return nullptr;
+  const at::Tensor* ws = argument(a[4], "workspace", at::kByte, {-1}, device, true);
+  if (!ws) return nullptr;
+  int page_size, tokens;
+  if (!integer(a[5], "page_size", &page_size) || !integer(a[6], "tokens", &tokens)) return nullptr;
+  if (sequences < 1 || sequences > INT_MAX - 1 || table->size(1) > INT_MAX || free_pages->numel() > INT_MAX || tokens < 0 ||
+      (sequences > 1 && table->stride(0) < table->size(1))) {
+    PyErr_SetString(PyExc_ValueError, "lengths, pages, free_pages or tokens is out of range");
+    return nullptr;
+  }
+  const int32_t* of[2] = {};
+  static const char* const names[2] = {"counts", "keep"};
+  for (int i = 0; i < 2; ++i) {
+    if (a[7 + i] == Py_None) continue;
+    const at::Tensor* t = argument(a[7 + i], names[i], at::kInt, {sequences}, device, true);
+    if (!t) return nullptr;
+    of[i] = static_cast<const int32_t*>(t->data_ptr());
+  }
+  std::optional<c10::cuda::CUDAGuard> on_device;
+  std::optional<c10::cuda::CUDAStreamGuard> on_stream;
+  void* stream;
+  if (!on_stream_of(a[12], device.index(), &stream, &on_device, &on_stream)) return nullptr;
+  at::Tensor starts, slots, positions;
+  if (!vector_output(a[9], sequences + 1, at::kInt, device, "starts", &starts) ||
+      !vector_output(a[10], tokens, at::kLong, device, "slots", &slots) ||
+      !vector_output(a[11], tokens, at::kInt, device, "positions", &positions))
+    return nullptr;
+  marlin_kv_pages c{};
+  c.table = static_cast<int32_t*>(table->data_ptr());
+  c.table_stride = sequences > 1 ? table->stride(0) : table->size(1);
+  c.lengths = static_cast<int32_t*>(lengths->data_ptr());
+  c.free_pages = static_cast<int32_t*>(free_pages->data_ptr());
+  c.free_count = static_cast<int32_t*>(free_count->data_ptr());
+  c.capacity = (int)free_pages->numel();
+  c.max_pages = (int)table->size(1);
+  c.sequences = (int)sequences;
+  c.page_size = page_size;
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = g_reserve(&c, of[0], of[1], tokens, static_cast<int32_t*>(starts.data_ptr()),
+                 tokens ? static_cast<int64_t*>(slots.data_ptr()) : nullptr, tokens ? static_cast<int32_t*>(positions.data_ptr()) : nullptr,
+                 ws->data_ptr(), (size_t)ws->numel(), stream);
+  Py_END_ALLOW_THREADS
+  if (st != 0) return finish(st, "marlin_kv_reserve", Py_None, at::Tensor());
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(starts)), THPVariable_Wrap(std::move(slots)), THPVariable_Wrap(std::move(positions)));
   CATCH
 }
 
@@ -606,6 +741,10 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_append = reinterpret_cast<decltype(g_append)>(address("marlin_kv_append"));
   g_attention = reinterpret_cast<decltype(g_attention)>(address("marlin_attention_decode"));
   g_block = reinterpret_cast<decltype(g_block)>(address("marlin_attention_block"));
+  g_append_scaled = reinterpret_cast<decltype(g_append_scaled)>(address("marlin_kv_append_scaled"));
+  g_attention_sinks = reinterpret_cast<decltype(g_attention_sinks)>(address("marlin_attention_sinks"));
+  g_block_sinks = reinterpret_cast<decltype(g_block_sinks)>(address("marlin_attention_block_sinks"));
+  g_reserve = reinterpret_cast<decltype(g_reserve)>(address("marlin_kv_reserve"));
   g_weight_bytes = reinterpret_cast<SizeFn>(address("marlin_packed_weight_bytes"));
   g_scale_bytes = reinterpret_cast<SizeFn>(address("marlin_packed_scale_bytes"));
   g_meta_bytes = reinterpret_cast<SizeFn2>(address("marlin_packed_meta_bytes"));
@@ -628,6 +767,7 @@ PyMethodDef methods[] = {
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(kv_append)), METH_FASTCALL, nullptr},
     {"attention_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attention_decode)), METH_FASTCALL, nullptr},
     {"attention_block", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attention_block)), METH_FASTCALL, nullptr},
+    {"kv_reserve", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(kv_reserve)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_binding", nullptr, -1, methods};
 
