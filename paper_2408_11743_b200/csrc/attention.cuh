@@ -418,10 +418,6 @@ __device__ __forceinline__ float power_above(float x) {
   const uint32_t bits = __float_as_uint(x), up = (bits & 0x7f800000u) + (bits & 0x7fffffu ? 0x800000u : 0u);
   return __uint_as_float(min(max(up, 0x800000u), 254u << 23));
 }
-__device__ __forceinline__ float finite_or_zero(float x) {  // its magnitude
-  x = fabsf(x);
-  return x <= 3.402823466e38f ? x : 0.f;
-}
 
 // ---- parts of an item in the workspace -----------------------------------------------------------
 // Rows of DP sums, their base, the sum of their weights, and two floats that are not used.  A CTA has parts of at most two

@@ -6,9 +6,10 @@
 // an e4m3 code loses nothing by it unless it becomes subnormal, one in two's complement at most half a step of the new scale, and however
 // often a block grows, the losses of a code add up to less than a step of its last scale (1/2 + 1/4 + ...).
 //
-// The tokens of one call in one block of one sequence are a run.  A CTA takes a run, or a part of its heads: one warp finds the scale of
-// one head's keys (or values) over all tokens of the run, so that nothing has to meet across warps, and the queries are shared out
-// to all threads.  Runs are numbered without a sum over the sequences: sequence b has the numbers from starts[b] / block + 2 b on, and n tokens
+// The tokens of one call in one block of one sequence are a run.  A CTA takes a run, or a part of its heads, and a team of its warps takes a
+// head at a time (one warp several heads, where a run has few tokens): so the scale of a head's keys or values over all tokens of
+// the run is found by a few warps, from registers that keep the elements until they are put away.  Queries go the same way without a
+// scale.  Runs are numbered without a sum over the sequences: sequence b has the numbers from starts[b] / block + 2 b on, and n tokens
 // lie in at most (n - 1) / block + 2 blocks, so no two sequences share a number; the numbers that nobody has end at once.
 #include "kv_cache.cuh"
 
@@ -16,7 +17,7 @@ namespace marlin_b200 {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kHold = 4;  // vectors (or pairs of them) of a lane that are read once; the rest are read again when the scale is known
+constexpr int kHold = 4;  // pairs of vectors of a lane that are read once; the rest are read again when the scale is known
 
 // What a CTA has to do: tokens rows [row, row + m) at positions [pos, pos + m), which lie in one block; rows [zero, row) have no position.
 struct Run {
@@ -24,22 +25,33 @@ struct Run {
   long long place, scale;  // of the first token, head 0 (in codes; -1: its page is not there) and of its block's scale
 };
 
-// unit j of a head that is turned: eight pairs (two vectors), or a vector
+// Unit j of a head, of head_dim / 16: two vectors of eight elements.  They are the two halves of eight pairs, or, where pairs lie side by
+// side and in what is not turned, two vectors of their own.
 struct Unit {
-  int at;     // element of the head where its (first) vector begins
-  bool pair;  // second vector at at + rotary_dim / 2
-  bool turned;
+  int at, second;  // elements of the head where the vectors begin
+  bool pair;
 };
-__device__ __forceinline__ Unit unit_of(const AppendParams& p, int j) {
+__device__ __forceinline__ Unit unit_of(const AppendParams& p, int j, bool turns) {
+  const int pairs = turns ? p.pair_units : 0, rest = p.cache.head_dim - pairs * 16;
   Unit r;
-  r.pair = j < p.pair_units;
-  r.at = r.pair ? j * 8 : p.pair_units * 16 + (j - p.pair_units) * 8;
-  r.turned = r.pair || r.at < p.rotary_dim;  // (pairs side by side: no pair units, the first rotary_dim elements)
+  r.pair = j < pairs;
+  r.at = r.pair ? j * 8 : pairs * 16 + (j - pairs) * 8;
+  r.second = r.at + (r.pair ? p.rotary_dim : rest) / 2;
   return r;
 }
 
-// x (and, of a pair unit, y) turned by the token's angles: `turn` has those of one unit `units` vectors apart, so that the lanes of a warp
-// read neighbouring ones
+// x and y turned by the token's angles: `turn` has those of one unit `units` vectors apart, so that the lanes of a warp read neighbouring ones
+__device__ __forceinline__ void rotate_side_by_side(const AppendParams& p, const float4* turn, int at, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; j += 4) {
+    const float4 cs = turn[j / 4 * (p.rotary_dim / 8) + at / 8];
+    const float a = x[j], d = x[j + 1], b = x[j + 2], e = x[j + 3];
+    x[j] = a * cs.x - d * cs.y;
+    x[j + 1] = d * cs.x + a * cs.y;
+    x[j + 2] = b * cs.z - e * cs.w;
+    x[j + 3] = e * cs.z + b * cs.w;
+  }
+}
 __device__ __forceinline__ void rotate(const AppendParams& p, const float4* turn, const Unit& r, float (&x)[8], float (&y)[8]) {
   if (r.pair) {
 #pragma unroll
@@ -51,26 +63,23 @@ __device__ __forceinline__ void rotate(const AppendParams& p, const float4* turn
       x[j + 1] = b * cs.z - e * cs.w;
       y[j + 1] = e * cs.z + b * cs.w;
     }
-  } else if (r.turned) {
-#pragma unroll
-    for (int j = 0; j < 8; j += 4) {
-      const float4 cs = turn[j / 4 * (p.rotary_dim / 8) + r.at / 8];
-      const float a = x[j], d = x[j + 1], b = x[j + 2], e = x[j + 3];
-      x[j] = a * cs.x - d * cs.y;
-      x[j + 1] = d * cs.x + a * cs.y;
-      x[j + 2] = b * cs.z - e * cs.w;
-      x[j + 3] = e * cs.z + b * cs.w;
-    }
+  } else if (!p.pair_units) {  // (no pair units: pairs side by side, or no rotation at all)
+    if (r.at < p.rotary_dim) rotate_side_by_side(p, turn, r.at, x);
+    if (r.second < p.rotary_dim) rotate_side_by_side(p, turn, r.second, y);
   }
 }
 
+// The largest magnitude of eight elements that is finite, and `top`.
 __device__ __forceinline__ float largest_of(const float (&x)[8], float top) {
+  float most = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float a = fabsf(x[j]);
-    top = fmaxf(top, a <= 3.402823466e38f ? a : 0.f);  // (what is not finite has no part in the scale)
+  for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]));  // (a NaN has no part in it)
+  if (most > 3.402823466e38f) {
+    most = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, finite_or_zero(x[j]));
   }
-  return top;
+  return fmaxf(top, most);
 }
 
 // four values -> four codes.  Infinities become the largest code; a NaN is 0 in two's complement, which has none.
@@ -103,10 +112,50 @@ __device__ __forceinline__ uint32_t shrunk(uint32_t w, float f) {
   return codes_of<INT8>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
 }
 
+// Cosines and sines of the angles position * inv_freq of m tokens from position pos on.  An angle is formed in 64 bits and reduced by whole
+// turns there: the rounding of a 32-bit product alone would be off by 2^-24 of it, half a percent of a radian at position 10^5.
+// Of many tokens those at every eighth position are formed, and the others turned on from these by the angles of one to seven positions,
+// which are formed alike: two factors and a product, each off by 2^-23 or so, for an eighth of the work and of the instructions, of which
+// sines were more than half.
+__device__ __forceinline__ float2 sine_of(double position, float frequency) {
+  constexpr double kTurnsPerRadian = 0.15915494309189533577;
+  const double turns = position * (double)frequency * kTurnsPerRadian;
+  float2 r;
+  sincospif((float)(2.0 * (turns - rint(turns))), &r.y, &r.x);
+  return r;
+}
+__device__ __forceinline__ void form_sines(const AppendParams& p, float4* turn, int pos, int m) {
+  __shared__ float2 on[7][128];
+  const int pairs = p.rotary_dim / 2, each = p.pair_units ? 4 : 2;
+  auto place = [&](int token, int pair) -> float2& {
+    const int v = pair / 2;
+    return reinterpret_cast<float2*>(&turn[token * (p.rotary_dim / 4) + v % each * (p.rotary_dim / 4 / each) + v / each])[pair % 2];
+  };
+  const bool few = m <= 8;
+  const int step = few ? 1 : 8, formed = (m + step - 1) / step;
+  for (int i = threadIdx.x; i < (formed + (few ? 0 : 7)) * pairs; i += kThreads) {
+    const int n = i / pairs, pair = i - n * pairs;
+    const float f = load(p.inv_freq + pair);
+    if (n < formed)
+      place(n * step, pair) = sine_of(pos + n * step, f);
+    else
+      on[n - formed][pair] = sine_of(n - formed + 1, f);
+  }
+  if (few) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < m * pairs; i += kThreads) {
+    const int token = i / pairs, pair = i - token * pairs;
+    if (token % 8 == 0) continue;
+    const float2 a = place(token & ~7, pair), b = on[token % 8 - 1][pair];
+    place(token, pair) = make_float2(a.x * b.x - a.y * b.y, a.y * b.x + a.x * b.y);
+  }
+}
+
 template <bool INT8>
 __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const AppendParams p) {
   extern __shared__ float4 turn[];  // of each token, two pairs (cosine, sine) a vector
   __shared__ Run run;
+  __shared__ float tops[2][kWarps];  // of the warps of a team
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const KvCacheView& c = p.cache;
@@ -147,73 +196,100 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
   if (run.m < 0) return;  // nobody's
   const int m = run.m, row = run.row, pos = run.pos;
 
-  for (int i = tid; i < m * (p.rotary_dim / 2); i += kThreads) {
-    constexpr double kTurnsPerRadian = 0.15915494309189533577;
-    const int token = i / (p.rotary_dim / 2), pair = i - token * (p.rotary_dim / 2);
-    const double turns = (double)(pos + token) * (double)load(p.inv_freq + pair) * kTurnsPerRadian;
-    float s, co;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &co);
-    const int v = pair / 2, each = p.pair_units ? 4 : 2;
-    reinterpret_cast<float2*>(&turn[token * (p.rotary_dim / 4) + v % each * (p.rotary_dim / 4 / each) + v / each])[pair % 2] = make_float2(co, s);
-  }
+  form_sines(p, turn, pos, m);
   __syncthreads();
 
-  // keys and values: a warp has the keys (or the values) of a head
+  // Where this lane stands: unit j of token first + i * pass of one of the `heads` heads that the warp has at a time.
+  const int units = c.head_dim / 16, per = 32 / units, tokens = max(1, min(m, per)), heads = per / tokens;
+  int team = 1;  // warps that have a head together: as many as keep all its tokens in registers
+  while (team < kWarps && team * per * kHold < m) team *= 2;
+  const int place = lane / units, j = lane - place * units, sub = place / tokens, pass = tokens * team;
+  const bool has = place < tokens * heads;  // (lanes that are left over have nothing)
+  const int mine = place - sub * tokens + warp % team * tokens, first = has ? mine : m;
+  // lanes that have the same head
+  const uint32_t together = (tokens * units == 32 ? ~0u : (1u << tokens * units) - 1) << sub * tokens * units;
   const int fill = pos & (block - 1);  // tokens that the block has already
-  for (int w = blockIdx.y * kWarps + warp; w < 2 * c.kv_heads && m > 0 && run.place >= 0; w += gridDim.y * kWarps) {
-    const bool key = w < c.kv_heads;
-    const int h = key ? w : w - c.kv_heads;
-    const int units = key ? p.head_units : c.head_dim / 8;
-    const int per = 32 / units, mine = lane / units, j = lane - mine * units;  // tokens a pass, and where this lane stands
-    Unit r = unit_of(p, j);
-    if (!key) {
-      r.at = j * 8;
-      r.pair = r.turned = false;
-    }
-    const long long stride = key ? p.k_stride : p.v_stride;
-    const uint16_t* const src = (key ? p.k : p.v) + row * stride + h * c.head_dim + r.at;
-    float* const scale_at = (key ? p.scales.k : p.scales.v) + run.scale + h * p.scales.s_head;
-    uint8_t* const base = static_cast<uint8_t*>(key ? c.k : c.v) + run.place + h * c.s_head;
-    const float old = fill ? load(scale_at) : 0.f;
+  const int q_groups = (p.q_heads + heads - 1) / heads, kv_groups = (c.kv_heads + heads - 1) / heads;
+  const int teams = kWarps / team;
+  int odd = 0;
+  for (int g = blockIdx.y * teams + warp / team; g < q_groups + 2 * kv_groups; g += gridDim.y * teams) {
+    const bool query = g < q_groups, key = !query && g < q_groups + kv_groups;
+    const int h = (query ? g : key ? g - q_groups : g - q_groups - kv_groups) * heads + sub;
+    const bool there = h < (query ? p.q_heads : c.kv_heads);
+    if (!query && (m == 0 || run.place < 0)) continue;  // (the same for the CTA)
+    const int begin = there ? first : m;
+    const Unit r = unit_of(p, j, query || key);
+    const long long stride = query ? p.q_stride : key ? p.k_stride : p.v_stride;
+    const uint16_t* const src = (query ? p.q : key ? p.k : p.v) + row * stride + h * c.head_dim;
     uint4 lo[kHold], hi[kHold];
-    const int first = mine < per ? mine : m;  // (lanes without a unit have no token)
-#pragma unroll
-    for (int i = 0; i < kHold; ++i) {
-      const int t = first + i * per;
-      if (t >= m) break;
-      lo[i] = load(reinterpret_cast<const uint4*>(src + t * stride));
-      if (r.pair) hi[i] = load(reinterpret_cast<const uint4*>(src + t * stride + p.rotary_dim / 2));
-    }
+    auto ask = [&](int t, uint4& a, uint4& b) {
+      a = load(reinterpret_cast<const uint4*>(src + t * stride + r.at));
+      b = load(reinterpret_cast<const uint4*>(src + t * stride + r.second));
+    };
     float x[8], y[8];
     auto turned = [&](int t, const uint4& a, const uint4& b) {
       to_floats(a, x);
-      if (r.pair) to_floats(b, y);
-      rotate(p, turn + t * (p.rotary_dim / 4), r, x, y);
+      to_floats(b, y);
+      if (query || key) rotate(p, turn + t * (p.rotary_dim / 4), r, x, y);
     };
-    auto again = [&](int t) {
-      const uint4 a = load(reinterpret_cast<const uint4*>(src + t * stride));
-      uint4 b = a;
-      if (r.pair) b = load(reinterpret_cast<const uint4*>(src + t * stride + p.rotary_dim / 2));
-      turned(t, a, b);
-    };
+    float* const scale_at = (key ? p.scales.k : p.scales.v) + run.scale + h * p.scales.s_head;
+    const float old = !query && fill && there ? load(scale_at) : 0.f;
+#pragma unroll
+    for (int i = 0; i < kHold; ++i)
+      if (begin + i * pass < m) ask(begin + i * pass, lo[i], hi[i]);
+
+    if (query) {
+      const long long out_stride = (long long)p.q_heads * c.head_dim;
+      uint16_t* const dst = p.q_out + h * c.head_dim;
+      if (there && has)
+        for (int t = run.zero + mine; t < row; t += pass) {  // (tokens without a position)
+          *reinterpret_cast<uint4*>(dst + t * out_stride + r.at) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(dst + t * out_stride + r.second) = make_uint4(0, 0, 0, 0);
+        }
+      for (int t0 = begin; t0 < m; t0 += kHold * pass) {
+        if (t0 != begin) {
+#pragma unroll
+          for (int i = 0; i < kHold; ++i)
+            if (t0 + i * pass < m) ask(t0 + i * pass, lo[i], hi[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kHold; ++i) {
+          const int t = t0 + i * pass;
+          if (t >= m) break;
+          turned(t, lo[i], hi[i]);
+          *reinterpret_cast<uint4*>(dst + (row + t) * out_stride + r.at) = to_halves(x);
+          *reinterpret_cast<uint4*>(dst + (row + t) * out_stride + r.second) = to_halves(y);
+        }
+      }
+      continue;
+    }
+
     float top = 0.f;
-    auto look = [&] {
-      top = largest_of(x, top);
-      if (r.pair) top = largest_of(y, top);
-    };
 #pragma unroll
     for (int i = 0; i < kHold; ++i) {
-      const int t = first + i * per;
+      const int t = begin + i * pass;
       if (t >= m) break;
       turned(t, lo[i], hi[i]);
-      look();
+      top = largest_of(y, largest_of(x, top));
     }
 #pragma unroll 2
-    for (int t = first + kHold * per; t < m; t += per) {
-      again(t);
-      look();
+    for (int t = begin + kHold * pass; t < m; t += pass) {
+      uint4 a, b;
+      ask(t, a, b);
+      turned(t, a, b);
+      top = largest_of(y, largest_of(x, top));
     }
-    top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));
+    if (heads == 1) {
+      top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));
+      if (team > 1) {
+        if (lane == 0) tops[odd][warp] = top;
+        named_bar_sync(1 + warp / team, team * 32);
+        for (int i = warp / team * team; i < warp / team * team + team; ++i) top = fmaxf(top, tops[odd][i]);
+        odd ^= 1;  // (the next head's go elsewhere: nobody is more than a barrier ahead)
+      }
+    } else if (has) {
+      top = __uint_as_float(__reduce_max_sync(together, __float_as_uint(top)));
+    }
 
     const float need = __fdiv_rn(top, INT8 ? 127.f : 448.f);
     const bool begun = fill && old > 0.f && old <= 3.402823466e38f;
@@ -222,58 +298,39 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
       now *= 2.f;
       shrink *= 0.5f;
     }
-    if (lane == 0 && !(fill && now == old)) *scale_at = now;
-    if (fill && shrink != 1.f) {  // what the block has is held under the new scale
-      const int vectors = c.head_dim / 8;
-      for (int i = lane; i < fill * vectors; i += 32) {
-        const int t = i / vectors;
-        uint2* const at = reinterpret_cast<uint2*>(base + (t - fill) * c.s_token + (i - t * vectors) * 8);
-        uint2 v = *at;
-        v.x = shrunk<INT8>(v.x, shrink);
-        v.y = shrunk<INT8>(v.y, shrink);
-        *at = v;
+    // (everybody has asked for the scale that was: those of a team before they met)
+    if (there && has && j == 0 && mine == 0 && !(fill && now == old)) *scale_at = now;
+    uint8_t* const base = static_cast<uint8_t*>(key ? c.k : c.v) + run.place + h * c.s_head;
+    if (fill && shrink != 1.f && there && has) {  // what the block has is held under the new scale
+      for (int t = mine; t < fill; t += pass) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint2* const at = reinterpret_cast<uint2*>(base + (t - fill) * c.s_token + (i ? r.second : r.at));
+          uint2 v = *at;
+          v.x = shrunk<INT8>(v.x, shrink);
+          v.y = shrunk<INT8>(v.y, shrink);
+          *at = v;
+        }
       }
     }
     const float inverse = now > 0.f ? __fdiv_rn(1.f, now) : 0.f;
     auto put = [&](int t) {
-      uint8_t* const to = base + t * c.s_token + r.at;
-      store_codes<INT8>(to, x, inverse);
-      if (r.pair) store_codes<INT8>(to + p.rotary_dim / 2, y, inverse);
+      store_codes<INT8>(base + t * c.s_token + r.at, x, inverse);
+      store_codes<INT8>(base + t * c.s_token + r.second, y, inverse);
     };
 #pragma unroll
     for (int i = 0; i < kHold; ++i) {
-      const int t = first + i * per;
+      const int t = begin + i * pass;
       if (t >= m) break;
       turned(t, lo[i], hi[i]);
       put(t);
     }
 #pragma unroll 2
-    for (int t = first + kHold * per; t < m; t += per) {
-      again(t);
+    for (int t = begin + kHold * pass; t < m; t += pass) {
+      uint4 a, b;
+      ask(t, a, b);
+      turned(t, a, b);
       put(t);
-    }
-  }
-
-  // queries: a thread has the same unit of every token
-  const int units = p.q_heads * p.head_units;
-  for (int u = blockIdx.y * kThreads + tid; u < units; u += gridDim.y * kThreads) {
-    const int head = u / p.head_units;
-    const Unit r = unit_of(p, u - head * p.head_units);
-    const uint16_t* const src = p.q + head * c.head_dim + r.at;
-    uint16_t* const dst = p.q_out + head * c.head_dim + r.at;
-    const long long out_stride = (long long)p.q_heads * c.head_dim;
-    for (int t = run.zero; t < row; ++t) {  // (tokens without a position)
-      *reinterpret_cast<uint4*>(dst + t * out_stride) = make_uint4(0, 0, 0, 0);
-      if (r.pair) *reinterpret_cast<uint4*>(dst + t * out_stride + p.rotary_dim / 2) = make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll 2
-    for (int t = 0; t < m; ++t) {
-      float x[8], y[8];
-      to_floats(load(reinterpret_cast<const uint4*>(src + (row + t) * p.q_stride)), x);
-      if (r.pair) to_floats(load(reinterpret_cast<const uint4*>(src + (row + t) * p.q_stride + p.rotary_dim / 2)), y);
-      rotate(p, turn + t * (p.rotary_dim / 4), r, x, y);
-      *reinterpret_cast<uint4*>(dst + (row + t) * out_stride) = to_halves(x);
-      if (r.pair) *reinterpret_cast<uint4*>(dst + (row + t) * out_stride + p.rotary_dim / 2) = to_halves(y);
     }
   }
 }
@@ -307,14 +364,17 @@ cudaError_t launch(const AppendParams& p, unsigned runs, unsigned parts, int sme
 cudaError_t launch_kv_append_blocks(AppendParams p, int interleaved, int sm_count, cudaStream_t stream) {
   p.rotary_dim = p.inv_freq ? p.rotary_dim : 0;
   p.pair_units = interleaved ? 0 : p.rotary_dim / 16;
-  p.head_units = p.pair_units + (p.cache.head_dim - p.pair_units * 16) / 8;
   const long long block = 1ll << p.scales.block_shift;
   const long long runs = p.starts ? p.tokens / block + 2ll * p.cache.sequences : p.cache.sequences;
   const int most = p.starts ? (int)(p.tokens < block ? p.tokens : block) : 1;  // tokens of a run
-  // the heads of a run are shared out to as many CTAs as give every SM eight of them, about
+  const int per = 32 / (p.cache.head_dim / 16);
+  int team = 1;
+  while (team < kWarps && team * per * kHold < most) team *= 2;
+  // the heads of a run are shared out to as many CTAs as give every SM eight of them, about (each forms the sines of the run for itself)
   const long long busy = p.starts ? p.tokens / block + p.cache.sequences : runs;
-  const long long units = (long long)p.q_heads * p.head_units;
-  const long long parts = max((units + kThreads - 1) / kThreads, (2ll * p.cache.kv_heads + kWarps - 1) / kWarps);
+  const int heads = most < per ? per / most : 1;
+  const long long groups = (p.q_heads + heads - 1) / heads + 2ll * ((p.cache.kv_heads + heads - 1) / heads);
+  const long long parts = (groups * team + kWarps - 1) / kWarps;
   const long long wanted = min(parts, (8ll * sm_count + busy - 1) / busy);
   const int smem = most * p.rotary_dim / 2 * 8;
   const auto run = p.scales.int8 ? launch<true> : launch<false>;

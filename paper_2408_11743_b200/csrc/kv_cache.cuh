@@ -83,6 +83,11 @@ __device__ __forceinline__ uint4 to_halves(const float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+__device__ __forceinline__ float finite_or_zero(float x) {  // its magnitude
+  x = fabsf(x);
+  return x <= 3.402823466e38f ? x : 0.f;
+}
+
 // bytes of a word of codes in two's complement -> fp16, exact: a code + 128 under the exponent of 1024, less 1152.
 // x: the word with its sign bits turned (int8_biased); `select`: which two bytes (0x4140: the lower ones, 0x4342: the upper ones)
 __device__ __forceinline__ uint32_t int8_biased(uint32_t word) { return word ^ 0x80808080u; }
