@@ -18,7 +18,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmarlin_b200.so")
 SOURCES = ["api.cu", "pack.cu", "pack_sparse.cu", "quantize.cu", "gemm_dense.cu", "gemm_tc.cu", "gemm_tc_dense.cu", "gemm_tc_sparse.cu",
-           "gemm_tc_w8.cu", "kv_append.cu", "kv_append_blocks.cu", "kv_reserve.cu", "attention.cu", "attention_more.cu", "attention_tc.cu", "attention_tc_more.cu"]
+           "gemm_tc_w8.cu", "kv_append.cu", "kv_append_blocks.cu", "kv_reserve.cu", "attention.cu", "attention_more.cu", "attention_tc.cu", "attention_tc_more.cu", "attention_prompt.cu"]
 HEADERS = [os.path.join(CSRC, "marlin_internal.cuh"), os.path.join(CSRC, "device_utils.cuh"), os.path.join(CSRC, "tc_utils.cuh"), os.path.join(CSRC, "gemm_tc.cuh"), os.path.join(CSRC, "tc_plan.h"), os.path.join(CSRC, "dense_plan.h"), os.path.join(CSRC, "kv_cache.cuh"), os.path.join(CSRC, "attention.cuh"), os.path.join(CSRC, "attention_warp.cuh"), os.path.join(CSRC, "attention_tc.cuh"), os.path.join(_ROOT, "include", "marlin_b200.h")]
 
 NVCC_FLAGS = [
@@ -110,7 +110,7 @@ def spill_report():
 TC_LAUNCH_REGS = 96  # kLaunchRegs of csrc/gemm_tc.cuh
 # kernels whose warps share out their registers, and how many a thread they are launched with: the same, Geometry::kLaunchRegs of
 # csrc/attention.cu, and all that 512 threads can have in csrc/attention_tc.cu (with blocks of 64 rows)
-LAUNCH_REGS = {"gemm_tc_kernel": TC_LAUNCH_REGS, "attention_kernel": 168, r"attention_tc_kernelILi\d+ELi64E": 128}
+LAUNCH_REGS = {"gemm_tc_kernel": TC_LAUNCH_REGS, "attention_kernel": 168, r"attention_tc_kernelILi\d+ELi64E": 128, "attention_prompt_kernel": 128}
 
 
 def check_registers(report):

@@ -200,6 +200,8 @@ cudaError_t launch_attention_tc(const AttentionParams& p, int sm_count, cudaStre
 // the same with sinks and with scales by block (attention_more.cu, attention_tc_more.cu); an 8-bit cache has its scales in p.scales
 cudaError_t launch_attention_more(const AttentionParams& p, int sm_count, cudaStream_t stream);
 cudaError_t launch_attention_tc_more(const AttentionParams& p, int sm_count, cudaStream_t stream);
+// many tokens a sequence, fp16, head_dim up to 128 (attention_prompt.cu; the choice is in attention_more.cu)
+cudaError_t launch_attention_prompt(const AttentionParams& p, int sm_count, cudaStream_t stream);
 
 // ---- the stripe partition (host and device use the same two formulas) ------------------------
 // worker w of P owns units [w*U/P, (w+1)*U/P); the owner of unit x is floor(((x+1)*P - 1) / U).
