@@ -42,11 +42,15 @@ struct Geometry {
   static constexpr int kConsumers = 8;               // warps that multiply (DP * NT / 4 sums a thread; twelve for 8 bits gained nothing)
   static constexpr int kGroups = kConsumers / (kParts * TW);
   static constexpr int kTeams = kConsumers / TW;     // warps that have the same rows
-  static constexpr int kProducers = 4;
+  // Warps that copy, in sets of four.  With scales by block a copying warp takes 1100 cycles for its part of a tile of 8 bits, most of them for the wait,
+  // the addresses and the scales, and not for the copies: two sets take every other stage.  (One set: 64 sequences of up to 8191 keys, 64 heads
+  // over 8, int8, 145 us; the warps that multiplied waited for most of it.)
+  static constexpr int kSets = kScaled && NT == 1 ? 2 : 1;
+  static constexpr int kProducers = 4 * kSets;
   static constexpr int kThreads = (kConsumers + kProducers) * 32;
   // The warps that copy hand registers to those that multiply, where these need more than the launch gives.
-  static constexpr int kLaunchRegs = 168, kProducerRegs = 88, kConsumerRegs = 208;
-  static_assert(kConsumers * kConsumerRegs + 4 * kProducerRegs <= (kConsumers + 4) * kLaunchRegs, "registers");
+  static constexpr int kLaunchRegs = kSets == 2 ? 128 : 168, kProducerRegs = 88, kConsumerRegs = kSets == 2 ? 168 : 208;
+  static_assert(kConsumers * kConsumerRegs + kProducers * kProducerRegs <= (kConsumers + kProducers) * kLaunchRegs, "registers");
   static constexpr int kRowBytes = DP * (F8 ? 1 : 2);
   static constexpr int kVectors = kRowBytes / 16;    // 16-byte vectors of a key
   static constexpr int kHalf = kTile * kRowBytes;    // the keys (or the values) of a tile
@@ -63,7 +67,8 @@ struct Geometry {
   static constexpr int kColumns = DP / kRounds;
   static constexpr int kJoin = kTeams * kRows * kColumns * 4;
   static constexpr int kRoom = 223 * 1024 - kOpen * kQBytes - kJoin;
-  static constexpr int kStages = kRoom / kStage > 16 ? 16 : kRoom / kStage;
+  static constexpr int kFit = kRoom / kStage > 16 ? 16 : kRoom / kStage;
+  static constexpr int kStages = kSets == 2 ? kFit / 2 * 2 : kFit;  // (as many for both sets)
   static constexpr int kSmem = kOpen * kQBytes + kJoin + kStages * kStage;
   static_assert(kConsumers % (kParts * TW) == 0 && kStages >= 2 && kStages >= kGroups && DP % (16 * kRounds) == 0, "ring");
 };
@@ -130,9 +135,14 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
   const int my_row = lane / G::kVectors, my_vec = lane % G::kVectors;
   const bool my_part = my_vec * (16 / kElement) < c.head_dim;
   const bool big_pages = c.page_shift >= 4;  // the sixteen keys of a part lie in one page
-  // the part of this warp; where there are fewer parts than warps, keys and values apart
-  const int part = producer % G::kParts;
-  const bool with_keys = G::kParts == G::kProducers || producer < G::kParts, with_values = G::kParts == G::kProducers || !with_keys;
+  // the set of this warp, and its part; where there are fewer parts than warps in a set, keys and values apart
+  const int set = producer / 4, part = producer % 4 % G::kParts;
+  const bool with_keys = G::kParts == 4 || producer % 4 < G::kParts, with_values = G::kParts == 4 || !with_keys;
+  // kScaled: the scales of a part, one for each block of its keys that begins in it or in front: lanes 0 - 15 those of keys, the others of values
+  const int entry_shift = min(p.scales.block_shift, 4), entry = lane & 15;
+  const bool my_scale = entry < 16 >> entry_shift && (lane < 16 ? with_keys : with_values);
+  const uint32_t scale_to = ((lane < 16 ? 0 : kTile) + part * 16 + entry) * 4;
+  const float* const scales = lane < 16 ? p.scales.k : p.scales.v;
   int stage = 0;
   uint32_t stage_phase = 1, segment = 0, slot_phase = 1;
   int slot = 0;
@@ -158,7 +168,10 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
     };
     const int batch = big_pages ? 32 : 1;
     const long long head_bytes = (x.h * c.s_head + my_row * c.s_token) * kElement + my_vec * 16;
+    // where the scale of the token at `key` lies, in the page with this number; -1: the page is not there
+    auto scale_place = [&](int page, int key) { return (unsigned)page < (unsigned)c.pages ? scale_offset(p, page, x.h, key) : -1ll; };
     int pages = page_of(0), pages_next = page_of(batch), in_batch = 0;
+    long long scale_at = -1;  // of the first scale of the part, in the lanes' tiles
     if (!arrived_at(sh, &sh.closed[slot], slot_phase, p.status)) break;
     if (lane == 0 && producer == 0) sh.segments[slot] = x;
     if (x.nt > 0) {  // Q; rows and elements that are not there are zeros
@@ -179,6 +192,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
       slot_phase ^= 1;
     }
     if (x.nt == 0) break;
+    if (G::kScaled && big_pages) scale_at = scale_place(pages, tile_of<EXTRA>(x, lane) * kTile + part * 16);
 
 #pragma unroll 1
     for (int i = 0; i < x.nt; ++i, ++in_batch) {
@@ -186,19 +200,63 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
         in_batch = 0;
         pages = pages_next;
         pages_next = page_of(i + batch);
+        if (G::kScaled && big_pages) scale_at = scale_place(pages, tile_of<EXTRA>(x, i + lane) * kTile + part * 16);
       }
-      if (!arrived_at(sh, &sh.empty[stage], stage_phase, p.status)) break;
+      if (G::kSets > 1 && (stage & 1) != set) {  // the other set's
+        if (++stage == G::kStages) {
+          stage = 0;
+          stage_phase ^= 1;
+        }
+        continue;
+      }
       const uint32_t to = ring + stage * G::kStage + part * 16 * G::kRowBytes;
       const int key0 = EXTRA != kNoExtra ? tile_of<EXTRA>(x, i) * kTile + part * 16 : key_first + i * kTile;
-      const int page = __shfl_sync(~0u, pages, in_batch);
-      if constexpr (G::kScaled) {  // lanes 0 - 15 a scale of a key each, the others of a value; zeros where nothing is asked for
-        const int key = key0 + (lane & 15), mine = __shfl_sync(~0u, pages, big_pages ? in_batch : lane & 15);
-        const bool there = seen_by_some<EXTRA>(p, key, low, high) && (unsigned)mine < (unsigned)c.pages;
-        const float* const scales = lane < 16 ? p.scales.k : p.scales.v;
-        const float* src = scales ? scales + (there ? scale_offset(p, mine, x.h, key) : 0) : &kScaleOfOne;
-        const uint32_t dst = ring + stage * G::kStage + 2 * G::kHalf + ((lane < 16 ? 0 : kTile) + part * 16 + (lane & 15)) * 4;
-        if (lane < 16 ? with_keys : with_values) copy4(dst, src, there);
+      if constexpr (G::kScaled) {  // (what does not need the stage comes before the wait for it)
+        const int page = __shfl_sync(~0u, pages, in_batch);
+        const int key = key0 + (entry << entry_shift);
+        const long long from = big_pages ? __shfl_sync(~0u, scale_at, in_batch)
+                                         : scale_place(__shfl_sync(~0u, pages, (entry << entry_shift) & 15), key & -(1 << p.scales.block_shift));
+        const bool scaled = from >= 0 && key < high && (key + (1 << entry_shift) > low || key < p.sinks);
+        const float* const scale = scales ? scales + (scaled ? from + (big_pages ? entry * p.scales.s_block : 0) : 0) : &kScaleOfOne;
+        const bool whole = big_pages && all_seen_by_some<EXTRA>(p, key0, 16, low, high) && (unsigned)page < (unsigned)c.pages;
+        const long long first = my_part && whole ? page * c.s_page + (key0 & ((1 << c.page_shift) - 1)) * c.s_token + head_bytes : 0;
+        const uint8_t* ks = static_cast<const uint8_t*>(c.k) + first;
+        const uint8_t* vs = static_cast<const uint8_t*>(c.v) + first;
+        const long long pass = my_part ? kPer * c.s_token : 0;
+        if (!arrived_at(sh, &sh.empty[stage], stage_phase, p.status)) break;
+        if (my_scale) copy4(ring + stage * G::kStage + 2 * G::kHalf + scale_to, scale, scaled);  // zeros where nothing is asked for
+        if (whole) {  // sixteen keys of one page: their places are s_token apart
+#pragma unroll
+          for (int r = 0; r < 16; r += kPer) {
+            const uint32_t dst = to + place<G::kVectors>(r + my_row, my_vec);
+            if (with_keys) copy16(dst, ks, my_part);
+            if (with_values) copy16(dst + G::kHalf, vs, my_part);
+            ks += pass;
+            vs += pass;
+          }
+        } else {
+#pragma unroll 1
+          for (int r = 0; r < 16; r += kPer) {
+            const int key = key0 + r + my_row;
+            const int mine = __shfl_sync(~0u, pages, big_pages ? in_batch : r + my_row);
+            const bool asked = seen_by_some<EXTRA>(p, key, low, high);
+            const long long from = asked ? cache_offset(c, mine, x.h, key, p.status) : -1;
+            const bool there = from >= 0 && my_part;
+            const long long bytes = there ? from + my_vec * 16 : 0;
+            const uint32_t dst = to + place<G::kVectors>(r + my_row, my_vec);
+            if (with_keys) copy16(dst, static_cast<const uint8_t*>(c.k) + bytes, there);
+            if (with_values) copy16(dst + G::kHalf, static_cast<const uint8_t*>(c.v) + bytes, there);
+          }
+        }
+        if (!withheld(p, producer == 0 && stage == 0)) copies_arrive(&sh.full[stage]);
+        if (++stage == G::kStages) {
+          stage = 0;
+          stage_phase ^= 1;
+        }
+        continue;
       }
+      if (!arrived_at(sh, &sh.empty[stage], stage_phase, p.status)) break;
+      const int page = __shfl_sync(~0u, pages, in_batch);
       if (big_pages && all_seen_by_some<EXTRA>(p, key0, 16, low, high) && (unsigned)page < (unsigned)c.pages) {
         // sixteen keys of one page: their places are s_token apart
         const long long first = (page * c.s_page + (key0 & ((1 << c.page_shift) - 1)) * c.s_token) * kElement + head_bytes;
@@ -382,11 +440,12 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
       // of this thread's keys g and g + 8
       float key_factor[2], value_scale[2];
       if constexpr (G::kScaled) {
-        const uint32_t scales = keys + 2 * G::kHalf + (part * 16 + g) * 4;
+        const int shift = min(p.scales.block_shift, 4);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          key_factor[i] = p.scale_log2 * __uint_as_float(lds32(scales + i * 32));
-          value_scale[i] = __uint_as_float(lds32(scales + kTile * 4 + i * 32));
+          const uint32_t at = keys + 2 * G::kHalf + (part * 16 + ((g + 8 * i) >> shift)) * 4;
+          key_factor[i] = p.scale_log2 * __uint_as_float(lds32(at));
+          value_scale[i] = __uint_as_float(lds32(at + kTile * 4));
           over |= finite_or_zero(value_scale[i]) > unit;
         }
       }
@@ -621,7 +680,7 @@ __global__ void __launch_bounds__(Geometry<DP, NT, TW, F8, EXTRA>::kThreads, 1) 
   const uint32_t ring = smem_u32(join) + G::kJoin;
   if (threadIdx.x == 0) {
     for (int i = 0; i < G::kStages; ++i) {
-      mbar_init(&sh.full[i], 32 * G::kProducers);
+      mbar_init(&sh.full[i], 32 * 4);
       mbar_init(&sh.empty[i], G::kParts * TW);
     }
     for (int i = 0; i < G::kOpen; ++i) {
