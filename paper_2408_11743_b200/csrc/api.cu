@@ -702,7 +702,7 @@ int marlin_kv_reserve(const marlin_kv_pages* c, const int32_t* counts, const int
                       int32_t* positions, void* workspace, size_t workspace_bytes, marlin_stream stream) {
   if (!c || !c->table || !c->lengths || !c->free_pages || !c->free_count || !workspace) return MARLIN_ERR_NULL;
   if (c->page_size < 1 || (c->page_size & (c->page_size - 1)) || c->page_size > (1 << 30) || c->max_pages < 1 || c->table_stride < c->max_pages ||
-      c->sequences < 1 || c->capacity < 1 || tokens < 0 || tokens > (1 << 30))
+      c->sequences < 1 || c->sequences > (1 << 30) || c->capacity < 1 || tokens < 0 || tokens > (1 << 30))
     return MARLIN_ERR_SHAPE;
   const uintptr_t numbers = reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->lengths) |
                             reinterpret_cast<uintptr_t>(c->free_pages) | reinterpret_cast<uintptr_t>(c->free_count) |

@@ -178,3 +178,13 @@ def test_given_outputs_strided_tables_streams_and_refusals(marlin):
         with pytest.raises(TypeError):
             marlin.kv_reserve(**{**d, **wrong})
     assert marlin.read_status(p.ws) == 0
+
+
+def test_sums_that_run_full(marlin):
+    # more rows than numbers of 32 bits hold, in the first and in a later one of the chunks that are summed at a time
+    for at in (0, 700):
+        p = Pages(np.full(1200, 5), 16, 4, 300)
+        counts = np.zeros(1200, np.int64)
+        counts[at], counts[at + 1], counts[at + 3] = 2 ** 31 - 1, 2 ** 31 - 1, 7
+        counts[:at:3] = 12
+        p.step(marlin, 5000, counts, np.where(np.arange(1200) % 5 == 0, 0, 99), status=9)
