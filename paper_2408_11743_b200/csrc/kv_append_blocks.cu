@@ -113,41 +113,23 @@ __device__ __forceinline__ uint32_t shrunk(uint32_t w, float f) {
 }
 
 // Cosines and sines of the angles position * inv_freq of m tokens from position pos on.  An angle is formed in 64 bits and reduced by whole
-// turns there: the rounding of a 32-bit product alone would be off by 2^-24 of it, half a percent of a radian at position 10^5.
-// Of many tokens those at every eighth position are formed, and the others turned on from these by the angles of one to seven positions,
-// which are formed alike: two factors and a product, each off by 2^-23 or so, for an eighth of the work and of the instructions, of which
-// sines were more than half.
-__device__ __forceinline__ float2 sine_of(double position, float frequency) {
-  constexpr double kTurnsPerRadian = 0.15915494309189533577;
-  const double turns = position * (double)frequency * kTurnsPerRadian;
-  float2 r;
-  sincospif((float)(2.0 * (turns - rint(turns))), &r.y, &r.x);
-  return r;
-}
+// turns there: the rounding of a 32-bit product alone would be off by 2^-24 of it, half a percent of a radian at position 10^5.  Then the fast
+// functions of the hardware will do: off by 2^-21 between -pi and pi, a thousandth of the rounding of a query to fp16.  (A CTA
+// forms them for itself, 4096 for a run of 64 tokens with 64 pairs; with the exact functions that was more than half of its instructions.)
 __device__ __forceinline__ void form_sines(const AppendParams& p, float4* turn, int pos, int m) {
-  __shared__ float2 on[7][128];
   const int pairs = p.rotary_dim / 2, each = p.pair_units ? 4 : 2;
-  auto place = [&](int token, int pair) -> float2& {
-    const int v = pair / 2;
-    return reinterpret_cast<float2*>(&turn[token * (p.rotary_dim / 4) + v % each * (p.rotary_dim / 4 / each) + v / each])[pair % 2];
-  };
-  const bool few = m <= 8;
-  const int step = few ? 1 : 8, formed = (m + step - 1) / step;
-  for (int i = threadIdx.x; i < (formed + (few ? 0 : 7)) * pairs; i += kThreads) {
-    const int n = i / pairs, pair = i - n * pairs;
-    const float f = load(p.inv_freq + pair);
-    if (n < formed)
-      place(n * step, pair) = sine_of(pos + n * step, f);
-    else
-      on[n - formed][pair] = sine_of(n - formed + 1, f);
-  }
-  if (few) return;
-  __syncthreads();
-  for (int i = threadIdx.x; i < m * pairs; i += kThreads) {
-    const int token = i / pairs, pair = i - token * pairs;
-    if (token % 8 == 0) continue;
-    const float2 a = place(token & ~7, pair), b = on[token % 8 - 1][pair];
-    place(token, pair) = make_float2(a.x * b.x - a.y * b.y, a.y * b.x + a.x * b.y);
+  if (pairs == 0) return;
+  // a thread has one pair (or, of more than there are threads, none) of every token that its group of threads has
+  const int group = (int)threadIdx.x / pairs, groups = kThreads / pairs, pair = (int)threadIdx.x - group * pairs;
+  if (group >= groups) return;
+  constexpr double kTurnsPerRadian = 0.15915494309189533577;
+  const double turns_each = (double)load(p.inv_freq + pair) * kTurnsPerRadian;
+  const int v = pair / 2;
+  float2* const to = reinterpret_cast<float2*>(&turn[v % each * (p.rotary_dim / 4 / each) + v / each]) + pair % 2;
+  for (int t = group; t < m; t += groups) {
+    const double turns = (double)(pos + t) * turns_each;
+    const float angle = (float)(turns - rint(turns)) * 6.283185307179586f;
+    to[t * (p.rotary_dim / 2)] = make_float2(__cosf(angle), __sinf(angle));
   }
 }
 
