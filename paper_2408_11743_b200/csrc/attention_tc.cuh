@@ -30,6 +30,11 @@
 
 namespace marlin_b200 {
 namespace {
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 
 constexpr int kTile = 128;
 constexpr int kLead = 4;                 // what an item costs beside its tiles, in tiles
@@ -209,7 +214,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
     // where this warp's half of tile i begins
     auto begin_of = [&](int i) { return EXTRA != kNoExtra ? tile_of<EXTRA>(x, i) * kTile + upper * 64 : key_first + i * kTile; };
     // where the four sixteens of this warp in eight tiles begin in the cache, a lane each, and in the next eight: the page number
-    // that was asked for, and what it comes to; -1 where it is not there
+    // that was asked for, and what it comes to; -1 where it is not there (of 8 bits: or not all of them are seen)
     auto key_of = [&](int i) { return begin_of(i + lane / 4) + lane % 4 * 16; };
     auto page_of = [&](int i) {
       const int key = key_of(i);
@@ -218,7 +223,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
       return big_pages && x.nt > 0 && key < high && key + 16 > low ? load(table + (key >> c.page_shift)) : -1;
     };
     auto place_of = [&](int i, int page) {
-      return (unsigned)page < (unsigned)c.pages
+      return (unsigned)page < (unsigned)c.pages && (!G::F8 || all_seen_by_some<EXTRA>(p, key_of(i), 16, low, high))
                  ? (page * c.s_page + x.h * c.s_head + (key_of(i) & ((1 << c.page_shift) - 1)) * c.s_token) * kElement : -1ll;
     };
     const int page_first = page_of(0);
@@ -257,13 +262,13 @@ __device__ __forceinline__ void produce(const AttentionParams& p, TcShared<G>& s
       const int n = 4 * x.nt;
       auto ask = [&](int q, uint32_t to) {  // (in_batch: its tile; a group of copies even where nothing is left to ask for)
         if (q < n) {
-          const int key0 = begin_of(q >> 2) + (q & 3) * 16;
           const long long place = __shfl_sync(~0u, places, in_batch * 4 + (q & 3));
-          if (place >= 0 && all_seen_by_some<EXTRA>(p, key0, 16, low, high)) {
+          if (place >= 0) {
             const uint8_t* src = cache + (part8 ? place + bytes8 : 0);
 #pragma unroll
             for (int j = 0; j < kPasses; ++j, src += pass8) copy16(to + j * 512, src, part8);
           } else {
+            const int key0 = begin_of(q >> 2) + (q & 3) * 16;
 #pragma unroll 1
             for (int j = 0; j < kPasses; ++j) {
               const int key = key0 + j * kPer8 + row8;
@@ -525,16 +530,19 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.s_free[buf]);
-      if constexpr (G::kScaled) {
+      const bool plain = G::kScaled && all && i > 0;  // (nothing to hide, no bases to look for: multiplied where the bases are subtracted)
+      if (G::kScaled && !plain) {
 #pragma unroll
         for (int r = 0; r < kMine; ++r) y[r] *= key_factor;
       }
+      auto hides = [&](int r) {
+        const int high = several ? sh.high[mine + r] : one_high;
+        return pos >= high || (p.window && pos < high - p.window && (EXTRA == kNoExtra || pos >= p.sinks));
+      };
       if (!all) {  // (a logit that becomes -inf whatever it is multiplied with)
 #pragma unroll
-        for (int r = 0; r < kMine; ++r) {
-          const int high = several ? sh.high[mine + r] : one_high;
-          if (pos >= high || (p.window && pos < high - p.window && (EXTRA == kNoExtra || pos >= p.sinks))) y[r] = hidden;
-        }
+        for (int r = 0; r < kMine; ++r)
+          if (hides(r)) y[r] = hidden;
       }
       if (i == 0) {  // bases to begin with: the largest logit of a row over the 32 keys of one warp, a quarter of the rows each
         bool none = false;
@@ -549,17 +557,36 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
             sh.base[mine + r + (warp & 3)] = top == kNone ? 0.f : top;
           }
         }
+        if constexpr (G::kScaled) {  // and the unit, which would move with the bases otherwise (3000 cycles)
+          const float top = warp_max(finite_or_zero(value_scale));
+          if (lane == 0) sh.scale_tops[warp] = top;
+        }
         fresh = any_of(1 + half, 128, none);
+        if constexpr (G::kScaled) {
+          const float* const tops = sh.scale_tops + half * 4;
+          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+          if (top > 0.f) {
+            unit = power_above(top);
+            inverse = 1.f / unit;
+          }
+        }
       }
       // logits in units of log2, relative to the bases; `over`: some are too far above, or there is no base yet
       float top = kNone;
+      const float times = plain ? key_factor : factor;
 #pragma unroll
       for (int r = 0; r < kMine; r += 4) {
         const float4 base = *reinterpret_cast<const float4*>(&sh.base[mine + r]);
-        y[r] = fmaf(y[r], factor, -base.x);
-        y[r + 1] = fmaf(y[r + 1], factor, -base.y);
-        y[r + 2] = fmaf(y[r + 2], factor, -base.z);
-        y[r + 3] = fmaf(y[r + 3], factor, -base.w);
+        if constexpr (G::kScaled) {
+          const f32x2 t2 = pack2(times, times);
+          unpack2(fma2(pack2(y[r], y[r + 1]), t2, pack2(-base.x, -base.y)), y[r], y[r + 1]);
+          unpack2(fma2(pack2(y[r + 2], y[r + 3]), t2, pack2(-base.z, -base.w)), y[r + 2], y[r + 3]);
+        } else {
+          y[r] = fmaf(y[r], times, -base.x);
+          y[r + 1] = fmaf(y[r + 1], times, -base.y);
+          y[r + 2] = fmaf(y[r + 2], times, -base.z);
+          y[r + 3] = fmaf(y[r + 3], times, -base.w);
+        }
         top = fmaxf(fmaxf(fmaxf(top, y[r]), fmaxf(y[r + 1], y[r + 2])), y[r + 3]);
       }
       // by any row: weights of 0, whatever the bases are
@@ -635,6 +662,7 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
       // weights, rounded to fp16 for the product (kBelow in attention.cuh)
       wait(&sh.p_done[pb], (u / G::kPBuffers & 1) ^ 1);  // (those that were there are multiplied)
       const uint32_t w_to = weights + pb * G::kPBytes + key * G::kPRow;
+      const float value_factor = value_scale * inverse;
 #pragma unroll
       for (int r = 0; r < kMine; r += 8) {
         uint32_t w[4];
@@ -643,18 +671,28 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
           y[r + e] = exp2_fast(y[r + e]);
           y[r + e + 1] = exp2_fast(y[r + e + 1]);
           if constexpr (G::kScaled) {  // (0 where a row does not see the key, also where its scale is not finite)
-            const float f = value_scale * inverse;
-            w[e / 2] = half2_bits(all || y[r + e] != 0.f ? y[r + e] * f : 0.f, all || y[r + e + 1] != 0.f ? y[r + e + 1] * f : 0.f);
+            float lo, hi;
+            unpack2(mul2(pack2(y[r + e], y[r + e + 1]), pack2(value_factor, value_factor)), lo, hi);
+            w[e / 2] = half2_bits(lo, hi);
           } else {
             w[e / 2] = half2_bits(y[r + e], y[r + e + 1]);
           }
           if (!G::kSumRows) {
-            l[r + e] += y[r + e];
-            l[r + e + 1] += y[r + e + 1];
+            if constexpr (G::kScaled) {
+              unpack2(add2(pack2(l[r + e], l[r + e + 1]), pack2(y[r + e], y[r + e + 1])), l[r + e], l[r + e + 1]);
+            } else {
+              l[r + e] += y[r + e];
+              l[r + e + 1] += y[r + e + 1];
+            }
           }
         }
         asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(w_to + (((mine + r) / 8) ^ swizzle_of<G::kPRow>(key)) * 16),
                      "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+      }
+      if (G::kScaled && !all && !(fabsf(value_factor) < INFINITY)) {  // (0 where a row does not see the key, also where its scale is not finite)
+#pragma unroll 1
+        for (int r = 0; r < kMine; ++r)
+          if (hides(r)) asm volatile("st.shared.u16 [%0], %1;" ::"r"(w_to + (((mine + r) / 8) ^ swizzle_of<G::kPRow>(key)) * 16 + (r & 7) * 2), "h"((uint16_t)0) : "memory");
       }
       tc_fence_before_sync();
       if (!G::kInt8 && several && !all && half == 0) {  // values of keys that not every row sees: what is not finite is left out
@@ -760,6 +798,16 @@ __device__ __forceinline__ void soften(const AttentionParams& p, TcShared<G>& sh
         float z[8];
         load_columns(lanes + 2 * N + r0, z);
         tc_wait_ld();
+        if (G::kScaled && !whole) {  // (rows that are not there have room, too)
+          if (key < DP) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) to_part[r * kLine + key] = z[r] * unit;
+          }
+          if (key < 8) *reinterpret_cast<float2*>(to_part + key * kLine + DP) = make_float2(sh.largest[r0 + key], sh.alpha[r0 + key]);
+          to_part += 8 * kLine;
+          __syncwarp();
+          continue;
+        }
 #pragma unroll
         for (int r = 0; r < 8; ++r)
           if (r0 + r < rows) give(r0 + r, z[r]);
