@@ -137,13 +137,14 @@ template <bool INT8>
 __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const AppendParams p) {
   extern __shared__ float4 turn[];  // of each token, two pairs (cosine, sine) a vector
   __shared__ Run run;
+  __shared__ int owner;
   __shared__ float tops[2][kWarps];  // of the warps of a team
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const KvCacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int shift = p.scales.block_shift, block = 1 << shift, id = blockIdx.x;
-  if (tid == 0) run.m = -1;
+  if (tid == 0) run.m = owner = -1;
   __syncthreads();
   // whose run this is: every thread looks at a sequence, and the one that has it follows the table
   for (int b = p.starts ? tid : id; b < (p.starts ? c.sequences : id + 1); b += kThreads) {
@@ -156,6 +157,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
       if (id < first || id >= next || from == to) continue;
       nth = (int)(id - first);
     }
+    if (atomicCAS(&owner, -1, b) != -1) continue;  // (only where begins descend, which they must not: one sequence, not parts of two)
     bool bad = false;
     const int len = cache_length(c, b, bad);
     if (bad && nth == 0) report_cache(p.status);
@@ -295,7 +297,8 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
         }
       }
     }
-    const float inverse = now > 0.f ? __fdiv_rn(1.f, now) : 0.f;
+    // (a scale below 2^-128 that was there before, over zeros: they stay zeros)
+    const float inverse = now > 0.f ? fminf(__fdiv_rn(1.f, now), 3.402823466e38f) : 0.f;
     auto put = [&](int t) {
       store_codes<INT8>(base + t * c.s_token + r.at, x, inverse);
       store_codes<INT8>(base + t * c.s_token + r.second, y, inverse);

@@ -299,3 +299,37 @@ def test_the_attention_half_of_a_layer(marlin, kind):
     q = marlin.kv_append(marlin.gemm(A, wq, sq, K, 768, G, two["workspace"]), **two, inv_freq=inv_freq)
     want = marlin.gemm(marlin.attention_decode(q, **two, window=64, sinks=4), wo, so, 512, N, G, two["workspace"])
     assert torch.equal(got, want) and torch.equal(one["k_cache"], two["k_cache"])
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_zeros_under_a_scale_whose_inverse_is_not_finite(marlin, kind):
+    # a block that was begun under 1e-40, and tokens of nothing but zeros: no code but 0
+    import torch
+    case = BlockCase([21, 5], [1, 2], 2, 2, 64, 32, kind, 16, seed=31)
+    case.qkv[:] = 0
+    d = case.dev(marlin)
+    d["k_scale"].fill_(1e-40), d["v_scale"].fill_(1e-40)
+    run(marlin, case, d=d)
+    for cache, scale in ((d["k_cache"], d["k_scale"]), (d["v_cache"], d["v_scale"])):
+        for b, (s, e) in enumerate(zip(case.starts[:-1], case.starts[1:])):
+            for at in range(int(case.lengths[b]) - int(e - s), int(case.lengths[b])):
+                page = int(case.table[b, at // 32])
+                assert not bits(cache[page, :, at % 32]).any()
+                assert (scale[page, :, at % 32 // 16] == scale.new_tensor(1e-40)).all()
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_begins_that_descend_are_contained(marlin, kind):
+    # (which they must not: what becomes of these sequences is open, but nothing else is touched)
+    import torch
+    case = BlockCase([300, 300, 300, 40], [100, 50, 50, 3], 2, 2, 64, 32, kind, 16, seed=32)
+    d = case.dev(marlin)
+    d["starts"].copy_(torch.tensor([0, 100, 50, 200, 203]))
+    before = [bits(d[x]).copy() for x in ("k_cache", "v_cache")]
+    q, _ = run(marlin, case, d=d)
+    mine = set(int(x) for b in range(4) for x in case.table[b, :-(-int(case.lengths[b]) // 32)])
+    others = [x for x in range(case.pages) if x not in mine]
+    for was, x in zip(before, ("k_cache", "v_cache")):
+        assert np.array_equal(bits(d[x])[others], was[others])
+    # the sequence behind them has what it asked for
+    assert np.array_equal(q[200:203].cpu().numpy().view(np.uint16), case.qkv[200:203, :case.q_heads * case.dim].view(np.uint16))
