@@ -365,7 +365,7 @@ typedef struct {
 
 /* marlin_kv_append into such a cache, whose scales are made on the way: nothing has to be measured beforehand.  With L the largest code (127;
  * 448 in e4m3) and a the largest magnitude of the new elements of a head in a block, after the rotation, that is finite:
- *   a block whose first token is among the new ones gets the scale s = a / L, whatever it held before;
+ *   a block whose first token is among the new ones gets the scale s = a / L, whatever it held before (in fp32, a times the number nearest to 1 / L);
  *   one that has tokens already keeps its scale if a / L <= s, otherwise s is doubled until that is so, and the codes of its earlier tokens
  *   are divided by the same power of two and rounded to nearest even (so a code loses at most a step of the block's last scale, however often
  *   that grew; nothing in e4m3 except where it becomes subnormal).  A scale that is not finite and above 0 stands for codes of 0.
@@ -414,7 +414,7 @@ typedef struct {
  * min(keep[b], lengths[b]) of them and gets counts[b] new ones behind these; lengths[b] becomes the sum.  (Drafted tokens that were not
  * accepted: keep is less than the length.  A sequence that ends: keep and count 0.)
  *   counts     device, int32 [sequences], or NULL: one each;   keep   device, int32 [sequences], or NULL: all
- *   tokens     rows of the step: at least the sum of the counts (0: none)
+ *   tokens     rows of the step: at least the sum of the counts (0: none).  2^30 tokens and 2^30 sequences are the most.
  *   starts     device, out, int32 [sequences + 1], or NULL: starts[b] = counts[0] + .. + counts[b - 1] (2^31 - 1 if that is less; negative
  *              counts are none), what the calls above take
  *   slots      device, out, int64 [tokens], or NULL: table[b][p / page_size] * page_size + p % page_size for the token at position p

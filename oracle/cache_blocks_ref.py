@@ -43,7 +43,7 @@ def append(codes, scales, new, sequence_pages, first, block):
             begin = at // block * block % page
             for h in range(codes.shape[1]):
                 a = np.abs(rows[:, h])
-                need = np.float32(np.max(np.where(np.isfinite(a), a, 0))) / largest
+                need = np.float32(np.max(np.where(np.isfinite(a), a, 0))) * (np.float32(1) / largest)
                 old = scales[number, h, part]
                 fill = at % block
                 begun = fill > 0 and np.isfinite(old) and old > 0
@@ -54,8 +54,8 @@ def append(codes, scales, new, sequence_pages, first, block):
                 if fill and shrink != 1:
                     kept = codes[number, h, begin:begin + fill]
                     codes[number, h, begin:begin + fill] = to((values(kept) * np.float64(shrink)).astype(np.float32))
-                inverse = np.float32(1) / now if now > 0 else np.float32(0)
                 with np.errstate(invalid="ignore", over="ignore"):
+                    inverse = min(np.float32(1) / now, np.finfo(np.float32).max) if now > 0 else np.float32(0)
                     codes[number, h, at % page:at % page + stop - at] = to(rows[:, h] * inverse)
         at = stop
 

@@ -109,7 +109,7 @@ def spill_report():
 
 TC_LAUNCH_REGS = 96  # kLaunchRegs of csrc/gemm_tc.cuh
 # kernels whose warps share out their registers, and how many a thread they are launched with: the same, Geometry::kLaunchRegs of
-# csrc/attention.cu, and all that 512 threads can have in csrc/attention_tc.cu (with blocks of 64 rows)
+# csrc/attention_warp.cuh, and all that 512 threads can have in csrc/attention_tc.cuh (with blocks of 64 rows) and csrc/attention_prompt.cu
 LAUNCH_REGS = {"gemm_tc_kernel": TC_LAUNCH_REGS, r"attention_kernelILi\d+ELi1ELi1ELb1ELi[12]E": 128, r"attention_kernelILi\d+ELi(1ELi1E(Lb0|Lb1ELi0E)|[24]E)": 168, r"attention_tc_kernelILi\d+ELi64E": 128, "attention_prompt_kernel": 128}
 
 

@@ -10,9 +10,15 @@
 // exponentials, 256 x 128 of them at 16 a cycle, 2048 cycles.  The halves take turns: one is multiplied while the other one's weights are
 // made.
 //
+// Measured, 64 heads over 8 of 128 elements, back to back in a graph: 1184 new tokens behind 8000 seen through a window of 6000, 229 us, 1015 TFLOP/s; a
+// prompt of 2048, 135 us; 700 tokens each of three prompts through a window of 512 with sinks, 105 us (its products alone 19, on
+// attention_tc.cuh 491): there an item has six or seven tiles, some of them seen in part, and costs some 8000 cycles for its first tile and its
+// end beside them, which no other item of the CTA hides.
+//
 // Warps: 0 - 3 the rows of the first half, 4 - 7 those of the second, 8 and 9 copy keys, 10 and 11 values (half of every tile each),
-// 12 and 13 issue the products of a half each, 14 and 15 bring Q and look through values that not every row sees.  Tensor memory: S (and the weights) of both halves, O of both.  Items (sequence, key head, block) are taken whole, every
-// CTA the one after the next grid: a prompt has many of them, and nothing has to be joined.
+// 12 and 13 issue the products of a half each, 14 and 15 bring Q and look through values that not every row sees.  Tensor memory: S (and the
+// weights) of both halves, O of both.  Items (sequence, key head, block) are taken whole, a CTA's next one lies a grid further on: a prompt
+// has many of them, and nothing has to be joined.
 #include "attention.cuh"
 #include "tc_utils.cuh"
 
@@ -23,7 +29,9 @@ constexpr int kTile = 128, kRows = 256, kHalf = 128;
 constexpr int kBlock = kTile * 128;  // 64 elements of the keys of a tile (or of the rows of a half): rows of 128 bytes, as the swizzle has them
 constexpr int kSoftmaxWarps = 8, kProducers = 4, kIssuers = 2, kCleaners = 2, kThreads = 512;
 constexpr int kStageRow = 80;        // bytes of a row of results on their way out: 32 of them, and room so that eight rows lie in different banks
-constexpr int kTurns = 12;           // tiles of an item from which on the halves take turns
+// Tiles of an item from which on the halves take turns: without them both run in step after some tiles and wait for each other (a window of 6000:
+// 283 us without, 247 with them), but items of few tiles end before that and wait for the turn instead (a window of 512: 64 and 72 us).
+constexpr int kTurns = 12;
 constexpr int kNotes = 2;            // items that can be open at a time
 // registers a thread: a softmax thread has a row of a tile, 128 logits
 constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
@@ -300,9 +308,10 @@ __device__ __forceinline__ void produce(const AttentionParams& p, PromptShared<G
 // ---- the threads that issue the products, one for each half ------------------------------------------
 // The products with the values of one tile and right behind them those with the keys of the next one (of the next item, where there is none):
 // products are executed in the order of their issue, so the new logits may take the place of the weights that are being multiplied, and
-// nobody waits in between.  The halves take turns: products of both in a mixed order would be done at the same time, and from then on both would have
-// their weights made at the same time and their products wait for each other, 5000 cycles a tile.  What else they need is waited for while the weights are made.  (A wait costs a thread some 190 cycles even where it is
-// over, an issue 65: one thread for both halves took 2400 cycles for each, and everybody waited for it.)
+// nobody waits in between.  The halves take turns: products of both in a mixed order would be done at the same time, and from then on both would
+// have their weights made at the same time and their products wait for each other, 5000 cycles a tile.  What else they need is waited for while
+// the weights are made.  (A wait costs a thread some 190 cycles even where it is over, an issue 65: one thread for both halves took 2400 cycles
+// for each, and everybody waited for it.)
 template <class G>
 __device__ __forceinline__ void multiply(const AttentionParams& p, PromptShared<G>& sh, uint32_t ring, uint32_t q_at, uint32_t tmem, int half) {
   const uint32_t logits_desc = instr_desc_f16(kHalf, kTile) | (p.scale_log2 < 0.f ? 1u << 13 : 0u);  // (bit 13: the left operand is negated)

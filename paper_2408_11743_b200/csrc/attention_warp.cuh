@@ -21,6 +21,9 @@
 // CTAs that end before others and in the joining of parts; one of 129 keys takes 5.8.  8-bit caches, 32 of 2000 to 4099 keys, 64 heads
 // over 8: 43 us, 4.7 TB/s, where the copies alone take 38.  No unit is full there (issue 36 %, ALU 32 %, tensor 13 %, DRAM 54 %): two warps
 // that multiply on each scheduler wait for what they convert and for what that is multiplied with.
+// With scales by block: 64 sequences of up to 8191 keys, 64 heads over 8, 128 us in two's complement, 117 in e4m3 (bytes alone 81); 64 of 2000 to
+// 4096, 32 heads, 366 and 329 (243); one of 129 keys 7.  What bounds these is the conversion in the warps that multiply, too: two
+// codes take one instruction in e4m3 and two (and a share in a third) in two's complement.
 #pragma once
 #include "attention.cuh"
 

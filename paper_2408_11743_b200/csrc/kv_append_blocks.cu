@@ -1,7 +1,7 @@
 // New keys and values into a paged cache of 8 bits with a scale for each block of tokens and key head, and the rotation of queries and keys.
 //
-// The scale of a block is s = a / L, a the largest magnitude in it and L the largest code (127 in two's complement, 448 in e4m3);
-// x is held as the code nearest to x * (1 / s).  A block that has tokens already keeps its scale while the new ones fit under s L.
+// The scale of a block is s = a / L (a times the fp32 number nearest to 1 / L), a the largest magnitude in it and L the largest code (127 in
+// two's complement, 448 in e4m3); x is held as the code nearest to x * (1 / s).  A block that has tokens already keeps its scale while the new ones fit under s L.
 // Otherwise s is doubled as often as that takes, and the codes that are there are divided by the same power of two and rounded once:
 // an e4m3 code loses nothing by it unless it becomes subnormal, one in two's complement at most half a step of the new scale, and however
 // often a block grows, the losses of a code add up to less than a step of its last scale (1/2 + 1/4 + ...).
@@ -11,6 +11,11 @@
 // the run is found by a few warps, from registers that keep the elements until they are put away.  Queries go the same way without a
 // scale.  Runs are numbered without a sum over the sequences: sequence b has the numbers from starts[b] / block + 2 b on, and n tokens
 // lie in at most (n - 1) / block + 2 blocks, so no two sequences share a number; the numbers that nobody has end at once.
+//
+// What bounds it: instructions.  Prompts of five sequences (10.8 thousand tokens, 32 heads and 32 key heads of 128, e4m3, blocks of 64, all
+// rotated): 108 us, 4.1 TB/s, where a copy of its bytes would take 67; keys are turned twice, to find the scale and to be put away, since they do not
+// fit into registers as 32-bit numbers.  Blocks of 16 take 106 us, of 4 tokens 204.  One token 3.9 us, 64 tokens 3.5: a launch.
+// (With the elements read again from the L2 in a second pass: 125 to 148 us for blocks of 64, 119 for 4.)
 #include "kv_cache.cuh"
 
 namespace marlin_b200 {
@@ -275,7 +280,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
       top = __uint_as_float(__reduce_max_sync(together, __float_as_uint(top)));
     }
 
-    const float need = __fdiv_rn(top, INT8 ? 127.f : 448.f);
+    const float need = top * (INT8 ? 1.f / 127.f : 1.f / 448.f);
     const bool begun = fill && old > 0.f && old <= 3.402823466e38f;
     float now = begun ? old : need, shrink = begun ? 1.f : 0.f;
     while (now < need) {

@@ -6,7 +6,9 @@
 // its tokens up among the begins of the chunk.  With many tokens several CTAs do the same sums and share the tokens out; lengths and the
 // stack of free pages, which all of them read, are written by the one that comes last.
 //
-// What bounds it: the latency of a launch, of a chain of three loads, the sums and a search.
+// What bounds it: the latency of a launch, of a chain of three loads, the sums and a search.  Measured, a step and the step that takes it back in a
+// graph: 64 sequences with a token each 10.0 us (5.0 a call), a thousand prompts of up to 700 tokens 41.4 (350 thousand slots and
+// positions, 4.2 MB; and eleven thousand pages that go back on the stack from one CTA).
 #include "kv_cache.cuh"
 
 namespace marlin_b200 {

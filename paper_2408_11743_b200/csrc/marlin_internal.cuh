@@ -119,7 +119,7 @@ cudaError_t launch_permute_zeros(uint8_t* z, uint16_t* zq, int K, int N, int G, 
 // canonical scales [K/G][N] <-> packed order (shared by the dense and the 2:4 pack)
 cudaError_t launch_permute_scales(uint16_t* s, uint16_t* sq, int K, int N, int G, bool inverse, cudaStream_t stream);
 
-// ---- the paged key-value cache (kv_append.cu, attention.cu) --------------------------------------
+// ---- the paged key-value cache (kv_append.cu, kv_append_blocks.cu, kv_reserve.cu, attention*.cu) --------------------------------------
 struct KvCacheView {
   void *k, *v;
   long long s_page, s_head, s_token;  // elements
@@ -195,7 +195,7 @@ struct AttentionParams {
 size_t attention_slot_bytes(int head_dim);
 cudaError_t launch_attention(const AttentionParams& p, int sm_count, cudaStream_t stream);
 // head_dim up to 128, where a key head has more than eight rows of an fp16 cache, or more than 32 of 128 elements of an 8-bit one
-// (launch_rows in attention.cu; the kernel is in attention_tc.cu)
+// (launch_rows in attention_warp.cuh; the kernel is in attention_tc.cuh)
 cudaError_t launch_attention_tc(const AttentionParams& p, int sm_count, cudaStream_t stream);
 // the same with sinks and with scales by block (attention_more.cu, attention_tc_more.cu); an 8-bit cache has its scales in p.scales
 cudaError_t launch_attention_more(const AttentionParams& p, int sm_count, cudaStream_t stream);

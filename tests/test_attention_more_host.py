@@ -134,7 +134,8 @@ def test_the_binding_refuses_what_is_not_on_a_gpu(marlin):
 def test_the_kernels_read_nothing_through_the_read_only_path():
     # they are resident while the kernel before them still writes what they read
     from paper_2408_11743_b200 import build
-    for name in ("kv_append_blocks.cu", "kv_reserve.cu", "attention_warp.cuh", "attention_tc.cuh", "attention_more.cu", "attention_tc_more.cu"):
+    for name in ("kv_append_blocks.cu", "kv_reserve.cu", "attention_warp.cuh", "attention_tc.cuh", "attention_more.cu", "attention_tc_more.cu",
+                 "attention_prompt.cu"):
         with open(os.path.join(build.CSRC, name)) as f:
             code = "\n".join(line.split("//")[0] for line in f)
         for word in ("__ldg", "ld.global.nc", "__restrict__"):

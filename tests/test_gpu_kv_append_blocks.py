@@ -333,3 +333,23 @@ def test_begins_that_descend_are_contained(marlin, kind):
         assert np.array_equal(bits(d[x])[others], was[others])
     # the sequence behind them has what it asked for
     assert np.array_equal(q[200:203].cpu().numpy().view(np.uint16), case.qkv[200:203, :case.q_heads * case.dim].view(np.uint16))
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_many_values_against_elementary_operations(marlin, kind):
+    # scales and codes of whole prompts bit for bit: amax times the fp32 number nearest to 1 / L, values times the fp32 inverse of that
+    import torch
+    case = BlockCase([1000, 777, 1500], [1000, 777, 1500], 16, 16, 128, 64, kind, 4, seed=33)
+    _, d = run(marlin, case)
+    x = torch.from_numpy(case.qkv).cuda().float().view(case.T, -1, 128)
+    for cache, scale, first in ((d["k_cache"], d["k_scale"], 16), (d["v_cache"], d["v_scale"], 32)):
+        for b, (s, e) in enumerate(zip(case.starts[:-1], case.starts[1:])):
+            at = torch.arange(int(e - s), device="cuda")
+            page = torch.from_numpy(case.table[b]).cuda().long()[at // 64]
+            new = x[int(s):int(e), first:first + 16]
+            runs = torch.nn.functional.pad(new, (0, 0, 0, 0, 0, -len(at) % 4)).unflatten(0, (-1, 4))
+            top = runs.abs().amax((1, 3)) * (torch.ones((), device="cuda") / (127 if kind == "int8" else 448))
+            assert torch.equal(scale[page, :, at % 64 // 4], top[at // 4])
+            y = new * (1 / top)[at // 4][..., None]
+            want = y.round().to(torch.int8) if kind == "int8" else y.to(torch.float8_e4m3fn)
+            assert torch.equal(cache[page, :, at % 64].view(torch.uint8), want.view(torch.uint8))
