@@ -12,8 +12,8 @@
 //
 // Measured, 64 heads over 8 of 128 elements, back to back in a graph: 1184 new tokens behind 8000 seen through a window of 6000, 229 us, 1015 TFLOP/s; a
 // prompt of 2048, 135 us; 700 tokens each of three prompts through a window of 512 with sinks, 105 us (its products alone 19, on
-// attention_tc.cuh 491): there an item has six or seven tiles, some of them seen in part, and costs some 8000 cycles for its first tile and its
-// end beside them, which no other item of the CTA hides.
+// attention_tc.cuh 491): there an item has six or seven tiles of 4900 cycles, 2000 for the products and 2900 for the softmax of both halves, 1400
+// more where some keys are hidden (a mask takes two instructions of half rate a logit), and 5500 at its end.
 //
 // Warps: 0 - 3 the rows of the first half, 4 - 7 those of the second, 8 and 9 copy keys, 10 and 11 values (half of every tile each),
 // 12 and 13 issue the products of a half each, 14 and 15 bring Q and look through values that not every row sees.  Tensor memory: S (and the
