@@ -142,7 +142,7 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
   const int set = producer / 4, part = producer % 4 % G::kParts;
   const bool with_keys = G::kParts == 4 || producer % 4 < G::kParts, with_values = G::kParts == 4 || !with_keys;
   // kScaled: the scales of a part, one for each block of its keys that begins in it or in front: lanes 0 - 15 those of keys, the others of values
-  const int entry_shift = min(p.scales.block_shift, 4), entry = lane & 15;
+  const int entry_shift = G::kScaled ? min(p.scales.block_shift, 4) : 0, entry = lane & 15;
   const bool my_scale = entry < 16 >> entry_shift && (lane < 16 ? with_keys : with_values);
   const uint32_t scale_to = ((lane < 16 ? 0 : kTile) + part * 16 + entry) * 4;
   const float* const scales = lane < 16 ? p.scales.k : p.scales.v;
@@ -163,8 +163,9 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
     auto page_of = [&](int i) {
       const int tile = big_pages ? i + lane : i;
       if constexpr (EXTRA != kNoExtra) {
-        const int key = tile_of<EXTRA>(x, tile) * kTile + part * 16 + (big_pages ? 0 : lane & 15);
-        return tile < x.nt && key < high && (key + (big_pages ? 16 : 1) > low || key < p.sinks) ? load(table + (key >> c.page_shift)) : INT_MIN;
+        // (the lane of a block's first key looks for the scale of the whole block: its page is asked for where a later key of the block is seen)
+        const int key = tile_of<EXTRA>(x, tile) * kTile + part * 16 + (big_pages ? 0 : lane & 15), last = big_pages ? key + 15 : key | ((1 << entry_shift) - 1);
+        return tile < x.nt && key < high && (last >= low || key < p.sinks) ? load(table + (key >> c.page_shift)) : INT_MIN;
       }
       const int key = key_first + tile * kTile + (big_pages ? 0 : lane & 15);
       return x.nt > 0 && key < high && key + (big_pages ? 16 : 1) > low ? load(table + (key >> c.page_shift)) : INT_MIN;
