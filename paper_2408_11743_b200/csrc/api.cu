@@ -669,8 +669,8 @@ static int attention_block(const void* A, const void* w_qkv, const void* s_qkv, 
   if (st == MARLIN_OK)
     st = check_attention(q, q_stride, cache, starts, M, q_heads, scale, window, O, workspace, workspace_bytes, &attention, scales,
                          sinks);
-  if (more) use_scales(&attention, cache, scales);
   if (st == MARLIN_OK) st = device_is_ours(&sm_count);
+  if (st == MARLIN_OK && more) use_scales(&attention, cache, scales);  // (scales that were refused are not looked at)
   if (st == MARLIN_OK)
     st = marlin_gemm(A, w_qkv, s_qkv, QKV, M, K, (int)columns, group_size, workspace, workspace_bytes, stream);
   if (st != MARLIN_OK) return st;
