@@ -368,9 +368,10 @@ typedef struct {
  *   a block whose first token is among the new ones gets the scale s = a / L, whatever it held before (in fp32, a times the number nearest to 1 / L);
  *   one that has tokens already keeps its scale if a / L <= s, otherwise s is doubled until that is so, and the codes of its earlier tokens
  *   are divided by the same power of two and rounded to nearest even (so a code loses at most a step of the block's last scale, however often
- *   that grew; nothing in e4m3 except where it becomes subnormal).  A scale that is not finite and above 0 stands for codes of 0.
+ *   that grew; nothing in e4m3 except where it becomes subnormal).  A scale that is not finite and above 0 stands for codes of 0, and for
+ *   no scale: the block gets s = a / L, and the codes of its earlier tokens become 0, those of NaN too.
  *   codes are the nearest (even) of x * (1 / s) in fp32; an infinity becomes the largest code, a NaN stays one in e4m3 and is 0 in two's
- *   complement; all codes are 0 where a is 0.
+ *   complement.  Where a is 0 and the block has no scale yet, s is 0 and all codes are 0, also those of infinities; a NaN stays one in e4m3.
  * Everything else as marlin_kv_append.  The same inputs give the same bits on every call; a prompt in two calls can give other ones than in one. */
 MARLIN_API int marlin_kv_append_scaled(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             void* q_out, const marlin_kv_cache* cache, const marlin_kv_scales* scales, const int32_t* starts, int tokens,

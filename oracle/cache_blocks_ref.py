@@ -53,10 +53,14 @@ def append(codes, scales, new, sequence_pages, first, block):
                 scales[number, h, part] = now
                 if fill and shrink != 1:
                     kept = codes[number, h, begin:begin + fill]
-                    codes[number, h, begin:begin + fill] = to((values(kept) * np.float64(shrink)).astype(np.float32))
+                    # (a scale that is not finite and above 0 stands for codes of 0, whatever they are)
+                    codes[number, h, begin:begin + fill] = to((values(kept) * np.float64(shrink)).astype(np.float32)) if begun else 0
                 with np.errstate(invalid="ignore", over="ignore"):
-                    inverse = min(np.float32(1) / now, np.finfo(np.float32).max) if now > 0 else np.float32(0)
-                    codes[number, h, at % page:at % page + stop - at] = to(rows[:, h] * inverse)
+                    if now > 0:
+                        y = rows[:, h] * min(np.float32(1) / now, np.finfo(np.float32).max)
+                    else:  # nothing that is finite and not 0: codes of 0, but for NaN
+                        y = np.where(np.isnan(rows[:, h]), rows[:, h], np.float32(0))
+                    codes[number, h, at % page:at % page + stop - at] = to(y)
         at = stop
 
 

@@ -95,8 +95,13 @@ __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
   const int k = max(-127, min(127, __float2int_rn(c))), l = max(-127, min(127, __float2int_rn(d)));
   return __byte_perm(__byte_perm(i, j, 0x0040), __byte_perm(k, l, 0x0040), 0x5410);
 }
+// (f = 0: a scale of 0, under which infinities and zeros of either sign have the code 0; a NaN stays one)
 template <bool INT8>
-__device__ __forceinline__ void store_codes(uint8_t* to, const float (&x)[8], float f) {
+__device__ __forceinline__ void store_codes(uint8_t* to, float (&x)[8], float f) {
+  if (f == 0.f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = x[j] != x[j] ? x[j] : 0.f;
+  }
   uint2 w;
   w.x = codes_of<INT8>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
   w.y = codes_of<INT8>(x[4] * f, x[5] * f, x[6] * f, x[7] * f);
@@ -295,9 +300,12 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           uint2* const at = reinterpret_cast<uint2*>(base + (t - fill) * c.s_token + (i ? r.second : r.at));
-          uint2 v = *at;
-          v.x = shrunk<INT8>(v.x, shrink);
-          v.y = shrunk<INT8>(v.y, shrink);
+          uint2 v = make_uint2(0, 0);  // (under a scale that is none every code stands for 0, a NaN's too)
+          if (begun) {
+            v = *at;
+            v.x = shrunk<INT8>(v.x, shrink);
+            v.y = shrunk<INT8>(v.y, shrink);
+          }
           *at = v;
         }
       }
