@@ -521,10 +521,11 @@ __device__ __forceinline__ void consume(const AttentionParams& p, Shared<G>& sh,
         float (&x)[4] = y[j][0];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+          // (0 where a row does not see the key, also where its scale is not finite; a weight that is 0 in fp32 is none of these)
+          const bool hidden = G::kScaled && !all && x[e] == kNone;
           x[e] = exp2_fast(x[e]);
           l[j][e & 1] += x[e];
-          // (0 where a row does not see the key, also where its scale is not finite)
-          if (G::kScaled) x[e] = all || x[e] != 0.f ? x[e] * (value_scale[e >> 1] * inverse) : 0.f;
+          if (G::kScaled) x[e] = hidden ? 0.f : x[e] * (value_scale[e >> 1] * inverse);
         }
         w[j][0] = transpose8x8(half2_bits(x[0], x[1]));
         w[j][1] = transpose8x8(half2_bits(x[2], x[3]));
