@@ -95,13 +95,8 @@ __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
   const int k = max(-127, min(127, __float2int_rn(c))), l = max(-127, min(127, __float2int_rn(d)));
   return __byte_perm(__byte_perm(i, j, 0x0040), __byte_perm(k, l, 0x0040), 0x5410);
 }
-// (f = 0: a scale of 0, under which infinities and zeros of either sign have the code 0; a NaN stays one)
 template <bool INT8>
-__device__ __forceinline__ void store_codes(uint8_t* to, float (&x)[8], float f) {
-  if (f == 0.f) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x[j] != x[j] ? x[j] : 0.f;
-  }
+__device__ __forceinline__ void store_codes(uint8_t* to, const float (&x)[8], float f) {
   uint2 w;
   w.x = codes_of<INT8>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
   w.y = codes_of<INT8>(x[4] * f, x[5] * f, x[6] * f, x[7] * f);
@@ -316,6 +311,23 @@ __global__ void __launch_bounds__(kThreads) kv_append_blocks_kernel(const Append
       store_codes<INT8>(base + t * c.s_token + r.at, x, inverse);
       store_codes<INT8>(base + t * c.s_token + r.second, y, inverse);
     };
+    // A scale of 0: infinities and zeros of either sign have the code 0, a NaN stays one.  (A loop of its own: looked for in `put` it cost
+    // prompts 3 %.)
+    if (now == 0.f) {
+#pragma unroll 1
+      for (int t = begin; t < m; t += pass) {
+        uint4 a, b;
+        ask(t, a, b);
+        turned(t, a, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] = x[i] != x[i] ? x[i] : 0.f;
+          y[i] = y[i] != y[i] ? y[i] : 0.f;
+        }
+        put(t);
+      }
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < kHold; ++i) {
       const int t = begin + i * pass;
