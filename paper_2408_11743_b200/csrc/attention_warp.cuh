@@ -261,7 +261,14 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
       }
       if (!arrived_at(sh, &sh.empty[stage], stage_phase, p.status)) break;
       const int page = __shfl_sync(~0u, pages, in_batch);
-      if (big_pages && all_seen_by_some<EXTRA>(p, key0, 16, low, high) && (unsigned)page < (unsigned)c.pages) {
+      // (Without sinks written out, here and below: through the functions the compiler takes another order, and 8-bit caches with up to eight rows a
+      // key head longer: 64 sequences of 1000 to 3000 keys, 32 heads, 190.5 us and 186.)
+      bool whole;
+      if constexpr (EXTRA == kNoExtra)
+        whole = big_pages && key0 >= low && key0 + 16 <= high && (unsigned)page < (unsigned)c.pages;
+      else
+        whole = big_pages && all_seen_by_some<EXTRA>(p, key0, 16, low, high) && (unsigned)page < (unsigned)c.pages;
+      if (whole) {
         // sixteen keys of one page: their places are s_token apart
         const long long first = (page * c.s_page + (key0 & ((1 << c.page_shift) - 1)) * c.s_token) * kElement + head_bytes;
         const uint8_t* ks = static_cast<const uint8_t*>(c.k) + (my_part ? first : 0);
@@ -280,7 +287,11 @@ __device__ __forceinline__ void produce(const AttentionParams& p, Shared<G>& sh,
         for (int r = 0; r < 16; r += kPer) {
           const int key = key0 + r + my_row;
           const int mine = __shfl_sync(~0u, pages, big_pages ? in_batch : r + my_row);
-          const bool asked = seen_by_some<EXTRA>(p, key, low, high);
+          bool asked;
+          if constexpr (EXTRA == kNoExtra)
+            asked = key >= low && key < high;
+          else
+            asked = seen_by_some<EXTRA>(p, key, low, high);
           const long long from = asked ? cache_offset(c, mine, x.h, key, p.status) : -1;
           const bool there = from >= 0 && my_part;
           const long long bytes = there ? from * kElement + my_vec * 16 : 0;
