@@ -372,7 +372,9 @@ typedef struct {
  *   no scale: the block gets s = a / L, and the codes of its earlier tokens become 0, those of NaN too.
  *   codes are the nearest (even) of x * (1 / s) in fp32; an infinity becomes the largest code, a NaN stays one in e4m3 and is 0 in two's
  *   complement.  Where a is 0 and the block has no scale yet, s is 0 and all codes are 0, also those of infinities; a NaN stays one in e4m3.
- * Everything else as marlin_kv_append.  The same inputs give the same bits on every call; a prompt in two calls can give other ones than in one. */
+ * Tokens that are taken back later (marlin_kv_reserve) leave the scale as they made it, and the codes of the tokens in front of them in its coarser steps.
+ * Sines and cosines are off by at most 2^-20 (2^-22 in marlin_kv_append, whose rotated queries can have other last bits).  Everything else as
+ * there.  The same inputs give the same bits on every call; a prompt in two calls can give other ones than in one. */
 MARLIN_API int marlin_kv_append_scaled(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                             void* q_out, const marlin_kv_cache* cache, const marlin_kv_scales* scales, const int32_t* starts, int tokens,
                             int q_heads, const float* inv_freq, int rotary_dim, int interleaved,
@@ -384,7 +386,10 @@ MARLIN_API int marlin_kv_append_scaled(const void* q, int64_t q_stride, const vo
  *   with scales by block the weights are rounded to fp16 together with the scales of their values, so a product w_j s_j is off by at most
  *   2^-11 of it, or 2^-31 of the largest weight of its row times the largest scale that it meets, if that is more;
  *   blocks of rows go only over tiles that some of their rows can see, so that a prompt with a window costs what the window holds;
- *   a scale that is not finite reaches the rows that see its tokens, and no others. */
+ *   a scale that is not finite reaches the rows that see its tokens, and no others.
+ * Many tokens a sequence over fp16 and up to 128 elements have a kernel of their own, here only: a prompt of 2048 tokens, 64 heads over 8 of 128 elements,
+ * 136 us (marlin_attention_decode: 0.6 ms).  Whether a call takes it goes by the mean of its tokens a sequence; sequences with one token each beside a
+ * prompt are right, but each of their key heads then costs a block of 256 rows that one CTA goes through alone. */
 MARLIN_API int marlin_attention_sinks(const void* q, int64_t q_stride, const marlin_kv_cache* cache, const marlin_kv_scales* scales,
                            const int32_t* starts, int tokens, int q_heads, float scale, int window, int sinks, void* out,
                            void* workspace, size_t workspace_bytes, marlin_stream stream);
@@ -413,7 +418,8 @@ typedef struct {
 
 /* Makes room for the new tokens of a step, and takes back what sequences do not need any more.  Sequence b with lengths[b] tokens keeps the first
  * min(keep[b], lengths[b]) of them and gets counts[b] new ones behind these; lengths[b] becomes the sum.  (Drafted tokens that were not
- * accepted: keep is less than the length.  A sequence that ends: keep and count 0.)
+ * accepted: keep is less than the length.  A sequence that ends: keep and count 0.  The scale of a block that drafts have made larger stays, see
+ * marlin_kv_append_scaled.)
  *   counts     device, int32 [sequences], or NULL: one each;   keep   device, int32 [sequences], or NULL: all
  *   tokens     rows of the step: at least the sum of the counts (0: none).  2^30 tokens and 2^30 sequences are the most.
  *   starts     device, out, int32 [sequences + 1], or NULL: starts[b] = counts[0] + .. + counts[b - 1] (2^31 - 1 if that is less; negative

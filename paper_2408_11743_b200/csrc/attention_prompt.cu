@@ -10,8 +10,8 @@
 // exponentials, 256 x 128 of them at 16 a cycle, 2048 cycles.  The halves take turns: one is multiplied while the other one's weights are
 // made.
 //
-// Measured, 64 heads over 8 of 128 elements, back to back in a graph: 1184 new tokens behind 8000 seen through a window of 6000, 229 us, 1015 TFLOP/s; a
-// prompt of 2048, 135 us; 700 tokens each of three prompts through a window of 512 with sinks, 105 us (its products alone 19, on
+// Measured, 64 heads over 8 of 128 elements, back to back in a graph: 1184 new tokens behind 8000 seen through a window of 6000, 231 us, 1008 TFLOP/s; a
+// prompt of 2048, 136 us; 700 tokens each of three prompts through a window of 512 with sinks, 105 us (its products alone 19, on
 // attention_tc.cuh 491): there an item has six or seven tiles of 4900 cycles, 2000 for the products and 2900 for the softmax of both halves, 1400
 // more where some keys are hidden (a mask takes two instructions of half rate a logit), and 5500 at its end.
 //
@@ -29,8 +29,9 @@ constexpr int kTile = 128, kRows = 256, kHalf = 128;
 constexpr int kBlock = kTile * 128;  // 64 elements of the keys of a tile (or of the rows of a half): rows of 128 bytes, as the swizzle has them
 constexpr int kSoftmaxWarps = 8, kProducers = 4, kIssuers = 2, kCleaners = 2, kThreads = 512;
 constexpr int kStageRow = 80;        // bytes of a row of results on their way out: 32 of them, and room so that eight rows lie in different banks
-// Tiles of an item from which on the halves take turns: without them both run in step after some tiles and wait for each other (a window of 6000:
-// 283 us without, 247 with them), but items of few tiles end before that and wait for the turn instead (a window of 512: 64 and 72 us).
+// Tiles of an item from which on the halves take turns: without them both run in step after some tiles and wait for each other (1184 tokens behind
+// 8000, a window of 6000: 267 us without, 231 with them), but items of few tiles end before that and wait for the turn instead (three prompts of 700
+// tokens behind 1000, a window of 512: 111 without, 119 with them).
 constexpr int kTurns = 12;
 constexpr int kNotes = 2;            // items that can be open at a time
 // registers a thread: a softmax thread has a row of a tile, 128 logits
